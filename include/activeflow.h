@@ -101,8 +101,10 @@ int af_set_option(af_ctx* ctx, int option, int value);
  * *flags receives the OR of AF_DEVERR_* bits set by kernels since the word was last cleared;
  * clear != 0 resets it.  AF_DEVERR_SPIN: a bounded wait inside the single-launch layer kernel
  * ran out (its results are invalid; set the workspace again before further calls).
- * AF_DEVERR_IDX: an index list broke its precondition (see af_set_validate). */
-enum { AF_DEVERR_SPIN = 1, AF_DEVERR_IDX = 2 };
+ * AF_DEVERR_IDX: an index list broke its precondition (see af_set_validate).
+ * AF_DEVERR_PAGED: a page table, length or row range of a paged batch cannot be right (see
+ * af_paged_batch). */
+enum { AF_DEVERR_SPIN = 1, AF_DEVERR_IDX = 2, AF_DEVERR_PAGED = 4 };
 int af_last_device_error(af_ctx* ctx, int* flags, int clear);
 
 /* Scratch memory.  af_workspace_bytes() gives the size that serves every call whose
@@ -308,6 +310,68 @@ int af_decode_layer_batch(af_ctx* ctx, const af_layer_cfg* cfg, const af_layer_w
                           const void* hidden_in, void* hidden_out, void* const* k_caches,
                           void* const* v_caches, const int* kv_len, int kv_cap, const int* pos,
                           const af_select_cfg* sel, af_idx_sets* sets, int32_t* union_n);
+
+/* ---- paged key-value cache: serving requests of any length -------------------------------
+ * The caches above hold one sequence each, in one piece.  Here all sequences share a pool of
+ * pages, and a table says which pages are whose; lengths and tables are device memory, so a
+ * captured step stays valid while the sequences grow.
+ *   k_pages, v_pages: fp16, page i at i * page_stride elements, inside a page [n_kv_heads]
+ *   [page_tokens][head_dim] (page_stride >= that, % 8 == 0; 16-byte aligned; K and V pages may
+ *   alternate in one allocation).  page_tokens: 16, 32, 64, 128 or 256.  head_dim 64 or 128. */
+typedef struct {
+  void *k_pages, *v_pages;
+  long long page_stride; /* elements */
+  int n_pages, page_tokens, n_kv_heads, head_dim;
+} af_paged_cache;
+
+/* The sequences of one call and their new tokens.  All pointers are device memory.
+ *   page_table [n_seqs][table_stride]: page of tokens [i * page_tokens, (i + 1) * page_tokens) of
+ *     a sequence at entry i; entries behind a sequence's last token are not read.
+ *   kv_len [n_seqs]: tokens of each sequence, the new ones included.
+ *   q_start [n_seqs + 1]: the new tokens of sequence b are rows [q_start[b], q_start[b+1]) of the
+ *     token tensors, its last q_start[b+1] - q_start[b] (0 or more, at most kv_len[b]) tokens in
+ *     order; rows behind q_start[n_seqs] are left as they are (a padded batch).  NULL: one new
+ *     token each, row b is sequence b's; a sequence with kv_len 0 then has none (a padded batch).
+ *   n_rows: rows of the token tensors; max_q_len: most rows of one sequence (a bound the host
+ *     knows; n_rows == n_seqs and max_q_len == 1 where q_start is NULL).
+ * A table entry outside [0, n_pages) that a token needs, a negative kv_len or one beyond the
+ * table, a row range that is negative, outside [0, n_rows], longer than max_q_len or than kv_len:
+ * reported (AF_DEVERR_PAGED) and not followed.  The token of such an entry is not stored and not
+ * seen; the rows of such a sequence are left as they are. */
+enum { AF_PAGED_MAX_SEQS = 1024, AF_PAGED_MAX_HEADS = 1024, AF_PAGED_MAX_ROWS = 1 << 22, AF_PAGED_MAX_TOKENS = 1 << 30 };
+typedef struct {
+  int n_seqs, table_stride, n_rows, max_q_len;
+  const int32_t *page_table, *kv_len, *q_start;
+} af_paged_batch;
+
+/* Appends the new tokens' keys and values.  qkv fp16 [n_rows][qkv_stride], a row = q (n_heads
+ * heads) | k | v (n_kv_heads each) of head_dim: the output of the fused projection.  Queries and
+ * keys: x <- x * rsqrt(mean(x^2) + eps) * gain for each head (where the gain, fp16 [head_dim], is
+ * not NULL), then the rotary embedding of af_decode_layer (pairs (i, i + head_dim/2), angle
+ * pos * rope_theta^(-2i/head_dim)) at pos[row] (int32 [n_rows]; NULL: the token's place in its
+ * sequence).  fp32 throughout, rounded once.  Keys and values go to their pages, the queries to
+ * q_out fp16 [n_rows][q_out_stride] (NULL: not stored; may be qkv with its stride).  Strides in
+ * elements, % 8 == 0; pointers 16-byte aligned.  Two sequences must not append to one page.
+ * The context's device must be the current HIP device (else AF_EINVAL); needs a workspace (for
+ * the error word). */
+int af_paged_append(af_ctx* ctx, const af_paged_cache* cache, const af_paged_batch* batch, int n_heads,
+                    float rope_theta, const void* q_gain_f16, const void* k_gain_f16, float eps,
+                    const int32_t* pos, const void* qkv_f16, long long qkv_stride, void* q_out_f16,
+                    long long q_out_stride);
+
+/* Attention of the new tokens over their sequences' pages (af_paged_append has stored them).
+ * q fp16 [n_rows][q_stride], out fp16 [n_rows][out_stride]: n_heads heads of head_dim each; query
+ * head h reads key head h / (n_heads / n_kv_heads).  A token at place p of its sequence sees the
+ * tokens j <= p (window == 0), or those of them with j > p - window or j < n_sink (the last
+ * `window`, and the first n_sink).
+ *   out = sum of softmax(scale * q.k_j) v_j over the tokens it sees, 0 if there are none
+ * (scale 0: 1 / sqrt(head_dim)).  Scores, softmax and sums are fp32.  Tokens that a row does not
+ * see do not enter its result, whatever their key and value hold.  The result depends on the batch
+ * (the split of the work follows the lengths) within rounding, and is the same from call to call.
+ * Alignment, device and workspace as af_paged_append; out must not overlap q. */
+int af_paged_attention(af_ctx* ctx, const af_paged_cache* cache, const af_paged_batch* batch, int n_heads,
+                       float scale, int window, int n_sink, const void* q_f16, long long q_stride,
+                       void* out_f16, long long out_stride);
 
 /* n_layers layers in sequence.  w, k_caches, v_caches, sets: host arrays of n_layers
  * entries.  With group > 1, layer l with l % group != 0 reuses the sets of its group's

@@ -26,7 +26,7 @@ AF_NOALLOC_MAX_OUT, AF_ENOALLOC_LIMIT = 65536, -6
 AF_OPT_LAYER_KERNEL, AF_OPT_VALIDATE, AF_OPT_TUNE_LX, AF_OPT_TUNE_WAVES = 1, 2, 3, 4
 AF_OPT_TUNE_SPLIT, AF_OPT_TUNE_WORKGROUPS, AF_OPT_MOE_ROUTER_KERNEL = 5, 6, 7
 AF_OPT_TUNE_ATTN_SPLITS, AF_OPT_TUNE_EARLY_ROWS = 8, 9
-AF_DEVERR_SPIN, AF_DEVERR_IDX = 1, 2
+AF_DEVERR_SPIN, AF_DEVERR_IDX, AF_DEVERR_PAGED = 1, 2, 4
 
 EXPORTS = [
     "af_create", "af_destroy", "af_set_stream", "af_strerror", "af_workspace_bytes",
@@ -40,6 +40,7 @@ EXPORTS = [
     "af_cost_eval", "af_plan_search", "af_sparse_gemv_f16_noalloc",
     "af_profile_set", "af_wall_clock_khz", "af_set_option", "af_last_device_error",
     "af_unpack_q4_g32", "af_probe_stream_read_variant", "af_decode_layer_batch",
+    "af_paged_append", "af_paged_attention",
 ]
 AF_MOE_MAX_EXPERTS, AF_MOE_MAX_TOP = 16, 4
 
@@ -111,6 +112,16 @@ class PlanOut(C.Structure):
                 ("hr", C.c_double), ("cost", CostOut)]
 
 
+class PagedCacheStruct(C.Structure):
+    _fields_ = [("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("page_stride", C.c_longlong),
+                ("n_pages", C.c_int), ("page_tokens", C.c_int), ("n_kv_heads", C.c_int), ("head_dim", C.c_int)]
+
+
+class PagedBatchStruct(C.Structure):
+    _fields_ = [("n_seqs", C.c_int), ("table_stride", C.c_int), ("n_rows", C.c_int), ("max_q_len", C.c_int),
+                ("page_table", C.c_void_p), ("kv_len", C.c_void_p), ("q_start", C.c_void_p)]
+
+
 _lib = None
 
 
@@ -151,6 +162,10 @@ def lib() -> C.CDLL:
         "af_decode_layer_batch": (i, [vp, C.POINTER(LayerCfg), C.POINTER(LayerWeights), i, vp, vp,
                                       C.POINTER(vp), C.POINTER(vp), C.POINTER(i), i, C.POINTER(i),
                                       C.POINTER(SelectCfg), C.POINTER(IdxSets), vp]),
+        "af_paged_append": (i, [vp, C.POINTER(PagedCacheStruct), C.POINTER(PagedBatchStruct), i, f, vp, vp, f, vp,
+                                vp, C.c_longlong, vp, C.c_longlong]),
+        "af_paged_attention": (i, [vp, C.POINTER(PagedCacheStruct), C.POINTER(PagedBatchStruct), i, f, i, i, vp,
+                                   C.c_longlong, vp, C.c_longlong]),
         "af_layer_tap": (i, [vp, i, C.POINTER(vp)]),
         "af_capture_begin": (i, [vp]),
         "af_capture_end": (i, [vp, C.POINTER(vp)]),
@@ -208,6 +223,52 @@ def _ptr(t, dtype=None, name="tensor"):
     if not t.is_contiguous():
         raise TypeError(f"{name} must be contiguous")
     return C.c_void_p(t.data_ptr())
+
+
+class PagedCache:
+    """af_paged_cache over two fp16 tensors [n_pages][n_kv_heads][page_tokens][head_dim] (contiguous inside a
+    page; the pages may lie further apart, both tensors alike).  Keeps the tensors alive."""
+
+    def __init__(self, k_pages, v_pages):
+        for t, name in ((k_pages, "k_pages"), (v_pages, "v_pages")):
+            if not t.is_cuda or t.dtype != torch.float16 or t.dim() != 4:
+                raise TypeError(f"{name} must be a CUDA tensor of fp16 with four dimensions")
+            n, kv, page, hd = t.shape
+            if t.shape != k_pages.shape or t.stride()[1:] != (page * hd, hd, 1) or \
+                    (n > 1 and t.stride(0) != k_pages.stride(0)):
+                raise TypeError(f"{name} must be contiguous inside a page, and shaped and spaced as k_pages")
+        if k_pages.device != v_pages.device:
+            raise TypeError("k_pages and v_pages must be on one device")
+        n, kv, page, hd = k_pages.shape
+        self.k_pages, self.v_pages, self.device = k_pages, v_pages, k_pages.device
+        self.n_kv_heads, self.head_dim = kv, hd
+        self.struct = PagedCacheStruct(k_pages.data_ptr(), v_pages.data_ptr(),
+                                       k_pages.stride(0) if n > 1 else kv * page * hd, n, page, kv, hd)
+        self._ref = C.byref(self.struct)
+
+
+class PagedBatch:
+    """af_paged_batch: page_table int32 [n_seqs][table_stride], kv_len int32 [n_seqs] and, unless every sequence
+    has one new token, q_start int32 [n_seqs + 1] with n_rows and max_q_len (rows of the token tensors, most
+    rows of one sequence).  Keeps the tensors alive; their contents may change between calls."""
+
+    def __init__(self, page_table, kv_len, q_start=None, n_rows=None, max_q_len=None):
+        n_seqs = kv_len.numel()
+        if page_table.dim() != 2 or page_table.shape[0] != n_seqs:
+            raise TypeError("page_table must be [n_seqs][table_stride]")
+        if q_start is None:
+            n_rows, max_q_len = n_seqs if n_rows is None else n_rows, 1 if max_q_len is None else max_q_len
+        elif q_start.numel() != n_seqs + 1 or n_rows is None:
+            raise TypeError("q_start must have n_seqs + 1 entries, and n_rows be given with it")
+        self.page_table, self.kv_len, self.q_start, self.n_rows = page_table, kv_len, q_start, int(n_rows)
+        self.n_seqs, self.device = n_seqs, kv_len.device
+        if page_table.device != self.device or (q_start is not None and q_start.device != self.device):
+            raise TypeError("the tensors of a batch must be on one device")
+        self.struct = PagedBatchStruct(
+            n_seqs, page_table.shape[1], self.n_rows, int(self.n_rows if max_q_len is None else max_q_len),
+            _ptr(page_table, torch.int32, "page_table"), _ptr(kv_len, torch.int32, "kv_len"),
+            _ptr(q_start, torch.int32, "q_start"))
+        self._ref = C.byref(self.struct)
 
 
 class Context:
@@ -485,6 +546,54 @@ class Context:
             _ptr(hidden_out, torch.float16, "hidden_out"), _ptr(k_cache, torch.float16, "k_cache"),
             _ptr(v_cache, torch.float16, "v_cache"), kv_len, kv_cap, pos, C.byref(sel),
             C.byref(sets) if sets is not None else None, C.byref(route)), "af_decode_moe_layer")
+
+    # ---- paged cache -----------------------------------------------------------------
+    def _paged_rows(self, t, batch: PagedBatch, width: int, name: str):
+        """(address, row stride) of a token tensor [n_rows][...] whose rows are contiguous."""
+        if t.dtype != torch.float16 or t.device != self.device:
+            raise TypeError(f"{name} must be fp16 on the context's device")
+        n = t.shape[0]
+        if n < batch.n_rows or t.numel() != n * width:
+            raise TypeError(f"{name} must have at least {batch.n_rows} rows of {width}")
+        if n == 0:
+            return None, width
+        inner = t.stride()[1:]
+        if inner != (1,) and (t.dim() != 3 or inner != (t.shape[2], 1)):
+            raise TypeError(f"{name} must be contiguous inside a row")
+        return t.data_ptr(), t.stride(0) if n > 1 else width
+
+    def _paged_check(self, cache: PagedCache, batch: PagedBatch):
+        if cache.device != self.device or batch.device != self.device:
+            raise TypeError("cache and batch must be on the context's device")
+
+    def paged_append(self, cache: PagedCache, batch: PagedBatch, qkv, q_out, n_heads: int, rope_theta: float = 10000.0,
+                     q_gain=None, k_gain=None, eps: float = 1e-5, pos=None):
+        """Store the new tokens' keys and values in their pages.  qkv [n_rows][(n_heads + 2 kv heads) head_dim]; q_out
+        [n_rows][n_heads head_dim] (None: not stored; the q columns of qkv will do) receives the rotated queries."""
+        self._paged_check(cache, batch)
+        hd = cache.head_dim
+        src, src_ld = self._paged_rows(qkv, batch, (n_heads + 2 * cache.n_kv_heads) * hd, "qkv")
+        dst, dst_ld = (None, 0) if q_out is None else self._paged_rows(q_out, batch, n_heads * hd, "q_out")
+        for t, name in ((q_gain, "q_gain"), (k_gain, "k_gain")):
+            if t is not None and (t.numel() != hd or t.device != self.device):
+                raise TypeError(f"{name} must have {hd} entries on the context's device")
+        if pos is not None and (pos.numel() < batch.n_rows or pos.device != self.device):
+            raise TypeError(f"pos must have at least {batch.n_rows} entries on the context's device")
+        _check(lib().af_paged_append(self._h, cache._ref, batch._ref, n_heads, rope_theta,
+                                     _ptr(q_gain, torch.float16, "q_gain"), _ptr(k_gain, torch.float16, "k_gain"), eps,
+                                     _ptr(pos, torch.int32, "pos"), src, src_ld, dst, dst_ld), "af_paged_append")
+        return q_out
+
+    def paged_attention(self, cache: PagedCache, batch: PagedBatch, q, out, n_heads: int, window: int = 0,
+                        n_sink: int = 0, scale: float = 0.0):
+        """Attention of the batch's new tokens over their pages: q, out [n_rows][n_heads head_dim]."""
+        self._paged_check(cache, batch)
+        width = n_heads * cache.head_dim
+        src, src_ld = self._paged_rows(q, batch, width, "q")
+        dst, dst_ld = self._paged_rows(out, batch, width, "out")
+        _check(lib().af_paged_attention(self._h, cache._ref, batch._ref, n_heads, scale, window, n_sink, src, src_ld,
+                                        dst, dst_ld), "af_paged_attention")
+        return out
 
     def layer_tap(self, which: int, n: int):
         """fp16 view (a copy) of an inter-operator tensor of the last decode_layer call."""
