@@ -41,6 +41,27 @@ PAGED_HD size_t paged_offset(const PagedView& v, int page, int h, int j, int hea
   const int slot = j & ((1 << v.page_shift) - 1);
   return (size_t)page * (size_t)v.page_stride + (((size_t)h << v.page_shift) + slot) * head_dim;
 }
+// The keys that rows at the places p0 .. p1 of a sequence can see, in tiles of TK: tile i starts at key i TK for the
+// first tokens (i < sinks), at lo + (i - sinks) TK behind them.  Tiles do not overlap; their ends may hold keys
+// that a row does not see.  lo is a multiple of 16, so 16 keys from a tile's start on never lie in two pages.
+struct PagedTiles {
+  int sinks, lo, n;
+};
+template <int TK>
+PAGED_HD PagedTiles paged_tiles(int p0, int p1, int window, int n_sink) {
+  if (p1 < 0) return PagedTiles{0, 0, 0};
+  const int first = window > 0 && p0 - window + 1 > 0 ? p0 - window + 1 : 0;
+  int lo = first & ~15, sinks = ((n_sink < first ? n_sink : first) + TK - 1) / TK;
+  if (sinks * TK >= lo) sinks = lo = 0;
+  return PagedTiles{sinks, lo, sinks + (p1 - lo) / TK + 1};
+}
+template <int TK>
+PAGED_HD int paged_tile_start(const PagedTiles& t, int i) {
+  return i < t.sinks ? i * TK : t.lo + (i - t.sinks) * TK;
+}
+PAGED_HD bool paged_seen(int key, int place, int window, int n_sink) {
+  return key <= place && (window <= 0 || key > place - window || key < n_sink);
+}
 
 __device__ __forceinline__ void paged_report(const PagedView& v) {
   __hip_atomic_fetch_or(v.tickets + AF_TICKET_ERR, (int)AF_DEVERR_PAGED, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);

@@ -109,6 +109,15 @@ extern "C" long long offset(long long page_stride, int shift, int page, int h, i
   PagedView v{}; v.page_stride = page_stride; v.page_shift = shift;
   return (long long)paged_offset(v, page, h, j, hd);
 }
+template <int TK> static int tiles_of(int p0, int p1, int window, int n_sink, int* starts, int most) {
+  const PagedTiles t = paged_tiles<TK>(p0, p1, window, n_sink);
+  for (int i = 0; i < t.n && i < most; ++i) starts[i] = paged_tile_start<TK>(t, i);
+  return t.n;
+}
+extern "C" int tiles(int tk, int p0, int p1, int window, int n_sink, int* starts, int most) {
+  return tk == 128 ? tiles_of<128>(p0, p1, window, n_sink, starts, most) : tiles_of<64>(p0, p1, window, n_sink, starts, most);
+}
+extern "C" int seen(int key, int place, int window, int n_sink) { return paged_seen(key, place, window, n_sink); }
 """
 
 
@@ -149,3 +158,24 @@ def test_pages_and_offsets(host):
         for page, h, j in ((0, 0, 0), (7, kv - 1, 12345), (100000, 1, (1 << 30) - 1)):
             want = page * stride + ((h << shift) + j % (1 << shift)) * hd
             assert host.offset(stride, shift, page, h, j, hd) == want   # past 32 bits in a long cache
+
+
+@pytest.mark.parametrize("tk", [64, 128])
+def test_tiles_hold_every_key_that_is_seen_once(host, tk):
+    starts = (C.c_int * 4096)()
+    for p0, p1 in ((0, 0), (5, 5), (63, 64), (127, 127), (128, 128), (0, 300), (777, 777), (500, 900), (1000, 1015)):
+        for window in (0, 1, 2, 15, 16, 17, 64, 100, 128, 129, 500, 2 ** 31 - 1):
+            for sinks in (0, 1, 16, 64, 100, 129, 600, 2 ** 31 - 1):
+                n = host.tiles(tk, p0, p1, window, sinks, starts, 4096)
+                held = [k for i in range(n) for k in range(starts[i], starts[i] + tk)]
+                assert len(held) == len(set(held)) and all(starts[i] % 16 == 0 for i in range(n))
+                see = {j for p in (p0, p1) for j in range(p1 + 1) if host.seen(j, p, window, sinks)}
+                assert see <= set(held) and held[-1] >= p1 and starts[n - 1] <= p1
+                assert see == {j for p in (p0, p1) for j in range(p + 1) if not window or j > p - window or j < sinks}
+                wide = p1 + 1 if not window else min(p1 + 1, p1 - max(0, p0 - window + 1) + 1 + min(sinks, max(0, p0 - window + 1)))
+                assert n <= wide // tk + 3   # no tile that nothing needs, but for the ragged ends
+    assert host.tiles(tk, -1, -1, 0, 0, starts, 4096) == 0
+    far = 2 ** 30 - 1
+    assert host.tiles(tk, far, far, 2 ** 31 - 1, 2 ** 31 - 1, starts, 4096) == 2 ** 30 // tk
+    assert host.tiles(tk, far, far, 100, 2 ** 31 - 1, starts, 4096) == 2 ** 30 // tk
+    assert host.tiles(tk, far, far, 100, 4, starts, 4096) <= 4
