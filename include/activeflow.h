@@ -333,7 +333,7 @@ typedef struct {
  *     order; rows behind q_start[n_seqs] are left as they are (a padded batch).  NULL: one new
  *     token each, row b is sequence b's; a sequence with kv_len 0 then has none (a padded batch).
  *   n_rows: rows of the token tensors; max_q_len: most rows of one sequence (a bound the host
- *     knows; n_rows == n_seqs and max_q_len == 1 where q_start is NULL).
+ *     knows; n_rows == n_seqs and max_q_len == 1 where q_start is NULL).  n_rows * n_heads < 2^31.
  * A table entry outside [0, n_pages) that a token needs, a negative kv_len or one beyond the
  * table, a row range that is negative, outside [0, n_rows], longer than max_q_len or than kv_len:
  * reported (AF_DEVERR_PAGED) and not followed.  The token of such an entry is not stored and not

@@ -4,78 +4,7 @@
 // or j < n_sink.  o = sum_j e^{s_j} v_j / sum_j e^{s_j} over those, s_j = scale q.k_j.
 #include <math.h>
 
-#include "paged.h"
-
-struct PagedAttnParams {
-  PagedView v;
-  const half_t* q;   // [n_rows][q_stride]
-  half_t* out;       // [n_rows][out_stride]
-  long long q_stride, out_stride;
-  int n_heads, window, n_sink;
-  float scale2;      // scale * log2(e): the exponentials are powers of two
-};
-
-// One query head of one row by one wave, on the vector unit in fp32: the keys one after the other (a group of
-// HD / 8 lanes takes each), those that the row does not see are not looked at.
-template <int HD>
-__device__ __forceinline__ void paged_row(const PagedAttnParams& p, int b, int row, int place, int h) {
-  constexpr int LPK = HD / 8, KPW = AF_WAVE / LPK;
-  const PagedView& v = p.v;
-  const int lane = threadIdx.x & 63, g = lane / LPK, c0 = lane % LPK * 8;
-  const int kvh = h / (p.n_heads / v.n_kv);
-  const half8 qh = *reinterpret_cast<const half8*>(p.q + (size_t)row * p.q_stride + (size_t)h * HD + c0);
-  float q[8], acc[8], m = -INFINITY, l = 0.f;
-#pragma unroll
-  for (int c = 0; c < 8; ++c) {
-    q[c] = (float)qh[c] * p.scale2;
-    acc[c] = 0.f;
-  }
-  const int lo = p.window > 0 ? max(0, place - p.window + 1) : 0;
-  const int sinks = min(p.n_sink, lo), n = place + 1 - lo + sinks;  // seen keys: [0, sinks) and [lo, place]
-  bool any = false;
-  for (int i0 = 0; i0 < n; i0 += KPW) {
-    const int i = i0 + g, j = i < sinks ? i : i - sinks + lo;
-    const int page = i < n ? paged_page(v, b, j) : -1;
-    float s = -INFINITY;
-    half8 vh = {};
-    if (page >= 0) {
-      const size_t o = paged_offset(v, page, kvh, j, HD) + c0;
-      const half8 kh = *reinterpret_cast<const half8*>(v.k + o);
-      vh = *reinterpret_cast<const half8*>(v.v + o);
-      s = 0.f;
-#pragma unroll
-      for (int c = 0; c < 8; ++c) s += q[c] * (float)kh[c];
-    }
-#pragma unroll
-    for (int off = 1; off < LPK; off <<= 1) s += __shfl_xor(s, off, AF_WAVE);
-    if (page < 0) continue;
-    any = true;
-    const float mx = fmaxf(m, s), safe = mx == -INFINITY ? 0.f : mx;
-    const float corr = exp2f(m - safe), w = exp2f(s - safe);
-    m = mx;
-    l = l * corr + w;
-#pragma unroll
-    for (int c = 0; c < 8; ++c) acc[c] = acc[c] * corr + w * (float)vh[c];
-  }
-  // the groups of lanes
-  float M = m;
-#pragma unroll
-  for (int off = LPK; off < AF_WAVE; off <<= 1) M = fmaxf(M, __shfl_xor(M, off, AF_WAVE));
-  const float f = any ? exp2f(m - (M == -INFINITY ? 0.f : M)) : 0.f;
-  l *= f;
-#pragma unroll
-  for (int off = LPK; off < AF_WAVE; off <<= 1) l += __shfl_xor(l, off, AF_WAVE);
-  half8 o;
-  const bool seen = __any(any);
-#pragma unroll
-  for (int c = 0; c < 8; ++c) {
-    float a = any ? acc[c] * f : 0.f;
-#pragma unroll
-    for (int off = LPK; off < AF_WAVE; off <<= 1) a += __shfl_xor(a, off, AF_WAVE);
-    o[c] = seen ? (half_t)(a / l) : (half_t)0;
-  }
-  if (g == 0) *reinterpret_cast<half8*>(p.out + (size_t)row * p.out_stride + (size_t)h * HD + c0) = o;
-}
+#include "paged_attn.h"
 
 // ---- few rows: one pass over the keys, split over their length --------------------------------------------
 #define SPL_THREADS 256
@@ -375,26 +304,6 @@ __global__ __launch_bounds__(SPL_THREADS, 2) void paged_split_kernel(PagedSplitP
   }
 }
 
-// ---- many rows: a wave per row and query head -------------------------------------------------------------
-template <int HD>
-__global__ __launch_bounds__(256) void paged_rows_kernel(PagedAttnParams p, int short_q) {
-  const int lane = threadIdx.x & 63;
-  const long long item = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (item >= (long long)p.v.n_rows * p.n_heads) return;
-  const int row = (int)(item / p.n_heads), h = (int)(item % p.n_heads);
-  int b = -1;
-  for (int i = lane; i < p.v.n_seqs; i += AF_WAVE) {
-    const PagedSeq s = paged_seq(p.v, i);
-    if (s.row0 <= row && row < s.row0 + s.q_len) b = i;
-  }
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) b = max(b, __shfl_xor(b, off, AF_WAVE));
-  if (b < 0) return;
-  const PagedSeq s = paged_seq(p.v, b);
-  if (s.q_len <= short_q) return;
-  paged_row<HD>(p, b, row, s.len - s.q_len + row - s.row0, h);
-}
-
 template <int HD>
 static int launch_attention(af_ctx* ctx, const PagedAttnParams& a) {
   const int rep = a.n_heads / a.v.n_kv, short_q = rep < SPL_ROWS ? SPL_ROWS / rep : 1;
@@ -414,12 +323,7 @@ static int launch_attention(af_ctx* ctx, const PagedAttnParams& a) {
   const size_t lds = ((size_t)a.v.n_seqs + 1) * sizeof(unsigned long long) + (size_t)a.v.n_seqs * sizeof(PagedSeq);
   hipLaunchKernelGGL(paged_split_kernel<HD>, dim3((unsigned)wgs), dim3(SPL_THREADS), lds, ctx->stream, p);
   AF_LAUNCH_CHECK();
-  if (a.v.max_q_len > short_q) {
-    const long long items = (long long)a.v.n_rows * a.n_heads;
-    hipLaunchKernelGGL(paged_rows_kernel<HD>, dim3((unsigned)((items + 3) / 4)), dim3(256), 0, ctx->stream, a, short_q);
-    AF_LAUNCH_CHECK();
-  }
-  return AF_OK;
+  return a.v.max_q_len > short_q ? af_launch_paged_prompt(ctx, a, HD, short_q) : AF_OK;
 }
 
 extern "C" int af_paged_attention(af_ctx* ctx, const af_paged_cache* cache, const af_paged_batch* batch, int n_heads,

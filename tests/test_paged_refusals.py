@@ -69,6 +69,7 @@ def test_cache_and_batch(call):
     assert call(batch={"n_rows": 0}) == EWORKSPACE and call(batch={"n_rows": 0}, q=None) == EWORKSPACE
     assert call(heads=0) == EINVAL and call(heads=5) == ESHAPE and call(heads=-4) == EINVAL
     assert call(heads=1026) == EINVAL
+    assert call(batch={"n_rows": 1 << 22}, heads=512) == EINVAL
     assert call(ctx=None) == ENULL
     assert B.lib().af_paged_append(CTX, None, None, 4, 1e4, None, None, 1e-5, None, ONE, 512, ONE, 256) == ENULL
     assert B.lib().af_paged_attention(CTX, None, None, 4, 0.0, 0, 0, ONE, 256, ONE, 256) == ENULL
