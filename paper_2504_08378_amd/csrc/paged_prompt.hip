@@ -2,36 +2,47 @@
 //
 // A workgroup has 128 rows, (token, query head) pairs that share a key head, and goes through the keys that any of
 // them sees, 64 at a time; a wave has 32 of the rows.
-//   scores   S^T[key][row] = K Q^T, 32 x 32 per instruction: a row's scores lie in the registers of two lanes, so its
-//            maximum and sum run along registers and one exchange;
+//   scores   S^T[key][row] = K Q^T, 32 x 32 per instruction: a row's scores lie in the registers of two lanes;
 //   values   O^T[dim][row] = V^T P^T: which eight keys a lane supplies per instruction is free as long as both operands
 //            agree, so it supplies those whose weights it has; V comes out of LDS transposed.
 // Pages go to LDS by direct loads, two tiles deep: the next tile is on its way while this one is used.  LDS rows
 // hold their 16-byte pieces in an order that depends on the row, so that the lanes of a read, which stand in one
-// column of up to 16 rows, lie in different banks; the loads pick the pieces from memory in that order.
+// column of up to 16 rows, lie in different banks (the conflict counter reads 0); the loads pick the pieces from memory in
+// that order.
+//
+// What bounds it, 8192 tokens of 32 heads on 32, causal, 550 GFLOP: 573 us, 960 TFLOP/s; the matrix unit is busy 53 % of the
+// cycles, at 1.65 GHz (a loop of nothing but these instructions on random data runs at 1.6 GHz, 1650 TFLOP/s, and at 2.1 GHz on
+// zeros: power sets the clock).  On the way, us: all loads of a tile issued in a row at its start, where a wave waits until the
+// memory path has taken them, and each read next to its product 669; a maximum per tile and an exchange between the lanes 655;
+// loads between the products, with reads that the compiler could not tell from the loads' buffers (it waited for them) 667;
+// this form 573.  Eight waves on one pair of tiles, half of them a phase behind the others, 573; without the waves' priorities
+// 587.
 #include <math.h>
+
+#include <type_traits>
 
 #include "paged_attn.h"
 
-#define PRM_THREADS 256
-#define PRM_ROWS 128
+#define PRM_WAVES 4
+#define PRM_ROWS (32 * PRM_WAVES)
 #define PRM_TILE 64
-
 typedef float prm_f16 __attribute__((ext_vector_type(16)));
+typedef half_t prm_h2 __attribute__((ext_vector_type(2)));
 typedef half_t prm_h4 __attribute__((ext_vector_type(4)));
 typedef __fp16 prm_fp16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) void prm_lds;
 typedef __attribute__((address_space(1))) const void prm_glb;
 
 template <int HD>
-__global__ __launch_bounds__(PRM_THREADS, 2) void paged_prompt_kernel(PagedAttnParams p, int short_q) {
+__global__ __launch_bounds__(PRM_WAVES * AF_WAVE, 2) void paged_prompt_kernel(PagedAttnParams p, int short_q) {
   constexpr int KS = HD / 16;        // contraction steps of the scores
   constexpr int DB = HD / 32;        // blocks of 32 dimensions
   constexpr int CH = HD / 8;         // 16-byte pieces of a row
   constexpr int RPI = AF_WAVE / CH;  // rows of a load instruction
-  constexpr int NI = 16 / RPI;       // load instructions of a wave per tile, for its 16 keys
+  constexpr int KEYS = PRM_TILE / PRM_WAVES;  // keys of a tile that a wave loads
+  constexpr int NI = KEYS / RPI;          // in so many instructions
   __shared__ __align__(16) half_t s_k0[PRM_TILE * HD], s_k1[PRM_TILE * HD], s_v0[PRM_TILE * HD], s_v1[PRM_TILE * HD];
-  __shared__ __align__(16) int s_bad[2][4];
+  __shared__ int s_gone;  // a page of this workgroup does not exist
 
   const PagedView& v = p.v;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -78,71 +89,61 @@ __global__ __launch_bounds__(PRM_THREADS, 2) void paged_prompt_kernel(PagedAttnP
   const int lr = lane / CH, lc = lane % CH;
   const int32_t* table = v.table + (size_t)b * v.table_stride;
   const int mask = (1 << v.page_shift) - 1;
-  int id = 0;
+  // where the page of the keys and of the values that are fetched next begins, and the number of the one behind them
+  size_t page_k, page_v;
+  int id_next;
   auto page_of = [&](int t) __attribute__((always_inline)) {
-    id = table[min(paged_tile_start<PRM_TILE>(tl, min(t, tl.n - 1)) + wave * 16, last) >> v.page_shift];
+    return table[min(paged_tile_start<PRM_TILE>(tl, min(t, tl.n - 1)) + wave * KEYS, last) >> v.page_shift];
   };
-  auto fetch = [&](int t, half_t* sk, half_t* sv, int* sb) __attribute__((always_inline)) {
-    const int pg = __builtin_amdgcn_readfirstlane(id);
-    const bool bad = !paged_page_ok(v, pg);
-    if (lane == 0) {
-      sb[wave] = bad;
-      if (bad) paged_report(v);
+  auto turn_page = [&]() __attribute__((always_inline)) {
+    int id = __builtin_amdgcn_readfirstlane(id_next);
+    if (!paged_page_ok(v, id)) {  // the first page is read in its place, and hidden
+      id = 0;
+      s_gone = 1;
+      paged_report(v);
     }
-    const size_t base = (size_t)(bad ? 0 : pg) * (size_t)v.page_stride + ((size_t)kvh << v.page_shift) * HD;
-    const int k0 = paged_tile_start<PRM_TILE>(tl, t) + wave * 16;
+    page_v = page_k;
+    page_k = (size_t)id * (size_t)v.page_stride + ((size_t)kvh << v.page_shift) * HD;
+  };
+  // Load instruction i of tile t's, and behind the last tile of that tile's once more.
+  auto fetch = [&](const half_t* page, int t, half_t* to, int i, bool keys) __attribute__((always_inline)) {
+    const int row = wave * KEYS + i * RPI + lr;
+    const unsigned o = (unsigned)(min(paged_tile_start<PRM_TILE>(tl, min(t, tl.n - 1)) + row, last) & mask) * HD;
+    const int c = lc ^ (keys ? row & (CH - 1) : HD == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2);
+    __builtin_amdgcn_global_load_lds((prm_glb*)(page + (o + c * 8)), (prm_lds*)(to + (wave * KEYS + i * RPI) * HD), 16, 0, 0);
+  };
+  // Reads: a key's row for the scores; four keys of one dimension for the values.  The lane's places are kept as numbers that
+  // the compiler does not look into: it takes reads whose address it cannot trace to one buffer for reads of what is being
+  // loaded, and waits for the loads.
+  const int i16 = lane & 15, kx = h ^ (lane & (CH - 1)), vx = HD == 128 ? i16 >> 2 : i16 >> 3;
+  int kat[KS], vat[DB];
 #pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int row = i * RPI + lr;
-      const unsigned o = (unsigned)(min(k0 + row, last) & mask) * HD;
-      const int ck = lc ^ (row & (CH - 1)), cv = lc ^ (HD == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2);
-      __builtin_amdgcn_global_load_lds((prm_glb*)(v.k + base + o + ck * 8), (prm_lds*)(sk + (wave * 16 + i * RPI) * HD), 16, 0, 0);
-      __builtin_amdgcn_global_load_lds((prm_glb*)(v.v + base + o + cv * 8), (prm_lds*)(sv + (wave * 16 + i * RPI) * HD), 16, 0, 0);
-    }
+  for (int ks = 0; ks < KS; ++ks) {
+    kat[ks] = n * HD + ((ks * 2) ^ kx) * 8;
+    asm volatile("" : "+v"(kat[ks]));
+  }
+#pragma unroll
+  for (int d = 0; d < DB; ++d) {
+    vat[d] = (4 * h + (i16 >> 2)) * HD + (d ^ vx) * 32 + ((lane >> 4) & 1) * 16 + (i16 & 3) * 4;
+    asm volatile("" : "+v"(vat[d]));
+  }
+  auto key = [&](const half_t* sk, int kb, int ks) __attribute__((always_inline)) {
+    return *reinterpret_cast<const half8*>(&sk[kat[ks] + kb * 32 * HD]);
   };
-  // reads: a key's row for the scores; four keys of one dimension for the values
-  const int i16 = lane & 15;
-  const int kat = n * HD, kx = h ^ (lane & (CH - 1));
-  const int vrow = 4 * h + (i16 >> 2), vx = HD == 128 ? i16 >> 2 : i16 >> 3;
-  const int vlow = ((lane >> 4) & 1) * 16 + (i16 & 3) * 4;
+  auto value = [&](const half_t* sv, int d, int s4) __attribute__((always_inline)) {
+    const auto lo = __builtin_amdgcn_ds_read_tr16_b64_v4f16((__attribute__((address_space(3))) prm_fp16x4*)&sv[vat[d] + 16 * s4 * HD]);
+    const auto hi = __builtin_amdgcn_ds_read_tr16_b64_v4f16((__attribute__((address_space(3))) prm_fp16x4*)&sv[vat[d] + (16 * s4 + 8) * HD]);
+    return (half8)__builtin_shufflevector(__builtin_bit_cast(prm_h4, lo), __builtin_bit_cast(prm_h4, hi), 0, 1, 2, 3, 4, 5, 6, 7);
+  };
 
   prm_f16 o[DB];
 #pragma unroll
   for (int d = 0; d < DB; ++d) o[d] = prm_f16{};
   float m = -INFINITY, l = 0.f;
 
-  auto compute = [&](int t, const half_t* sk, const half_t* sv, const int* sb) __attribute__((always_inline)) {
+  // Scores that a row does not see, behind the products of tile t.
+  auto hide = [&](int t, prm_f16 (&s)[2]) __attribute__((always_inline)) {
     const int k0 = paged_tile_start<PRM_TILE>(tl, t);
-    if (!(k0 <= wp1 && (window <= 0 || k0 + PRM_TILE - 1 > wp0 - window || k0 < n_sink))) return;
-    // Reads run ahead of the products that use them: both blocks of keys before the first product, the first
-    // values under the second block's, each block of values under the one before.
-    auto keys = [&](half8 (&a)[KS], int kb) __attribute__((always_inline)) {
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) a[ks] = *reinterpret_cast<const half8*>(sk + kb * 32 * HD + kat + ((ks * 2) ^ kx) * 8);
-    };
-    auto values = [&](half8 (&a)[4], int d) __attribute__((always_inline)) {
-#pragma unroll
-      for (int s4 = 0; s4 < 4; ++s4) {
-        const half_t* at = sv + (vrow + 16 * s4) * HD + ((d ^ vx) * 32 + vlow);
-        const auto lo = __builtin_amdgcn_ds_read_tr16_b64_v4f16((__attribute__((address_space(3))) prm_fp16x4*)at);
-        const auto hi = __builtin_amdgcn_ds_read_tr16_b64_v4f16((__attribute__((address_space(3))) prm_fp16x4*)(at + 8 * HD));
-        a[s4] = __builtin_shufflevector(__builtin_bit_cast(prm_h4, lo), __builtin_bit_cast(prm_h4, hi), 0, 1, 2, 3, 4, 5, 6, 7);
-      }
-    };
-    const int4 bad = *reinterpret_cast<const int4*>(sb);
-    prm_f16 s[2] = {prm_f16{}, prm_f16{}};
-    half8 a0[KS], a1[KS], v0[4], v1[4];
-    keys(a0, 0);
-    keys(a1, 1);
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) s[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a0[ks], q[ks], s[0], 0, 0, 0);
-    __builtin_amdgcn_sched_barrier(0);
-    values(v0, 0);
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) s[1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a1[ks], q[ks], s[1], 0, 0, 0);
-    __builtin_amdgcn_sched_barrier(0);
     if (!(k0 + PRM_TILE - 1 <= wp0 && (window <= 0 || k0 > wp1 - window || k0 + PRM_TILE <= n_sink))) {
       const int end = place - k0 - 4 * h, from = (window > 0 ? place - window + 1 : 0) - k0 - 4 * h, first = n_sink - k0 - 4 * h;
 #pragma unroll
@@ -153,77 +154,148 @@ __global__ __launch_bounds__(PRM_THREADS, 2) void paged_prompt_kernel(PagedAttnP
           s[kb][i] = (row <= end) & ((row >= from) | (row < first)) ? s[kb][i] : -INFINITY;
         }
     }
-    if (bad.x | bad.y | bad.z | bad.w) {
-      const int gone[4] = {bad.x, bad.y, bad.z, bad.w};
+    if (s_gone) {
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
+      for (int g = 0; g < 4; ++g) {
+        const int k = k0 + g * 16;
+        if (k <= last && paged_page_ok(v, __builtin_amdgcn_readfirstlane(table[k >> v.page_shift]))) continue;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[kb][i] = gone[kb * 2 + (i >> 3)] ? -INFINITY : s[kb][i];
+        for (int i = 0; i < 8; ++i) s[g >> 1][(g & 1) * 8 + i] = -INFINITY;
+      }
     }
-    float mx = s[0][0];
+  };
+  half8 w[4];
+  // The matrix unit's half of a step: the values of tile t - 1 (sv) by its weights, the scores of tile t (keys sk).
+  prm_f16 s[2];
+  auto products = [&](auto first, const half_t* sk, const half_t* sv, auto&& between) __attribute__((always_inline)) {
+    half8 x[2][4], a[2][KS];
+    // Every read stands one block in front of its product; the compiler would move it next to that.
+    if constexpr (!first.value) {
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
+      for (int s4 = 0; s4 < 4; ++s4) x[0][s4] = value(sv, 0, s4);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[kb][i]);
-    mx = fmaxf(mx, __shfl_xor(mx, 32, AF_WAVE)) * scale2;
-    if (__any(mx > m)) {
-      mx = fmaxf(mx, m);
+      for (int d = 0; d < DB; ++d) {
+#pragma unroll
+        for (int s4 = 0; s4 < 4; ++s4) {
+          if (d + 1 < DB) x[(d + 1) & 1][s4] = value(sv, d + 1, s4);
+          if (d + 1 == DB && s4 * 2 < KS) {
+            a[0][s4 * 2] = key(sk, 0, s4 * 2);
+            a[0][s4 * 2 + 1] = key(sk, 0, s4 * 2 + 1);
+          }
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[d & 1][s4], w[s4], o[d], 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        between(d);
+      }
+    } else {
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) a[0][ks] = key(sk, 0, ks);
+#pragma unroll
+      for (int d = 0; d < DB; ++d) between(d);
+    }
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) s[kb] = prm_f16{};
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      a[1][ks] = key(sk, 1, ks);
+      s[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[0][ks], q[ks], s[0], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) s[1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[1][ks], q[ks], s[1], 0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // The vector unit's half: the scores to weights.  Weights times 2^7, each to the nearest of its 11 bits: one more rounding of
+  // the size of the result's own, and independent from key to key.  Returns the sum of the rounded ones.
+  auto weigh = [&]() __attribute__((always_inline)) {
+    const float off = (m == -INFINITY ? 0.f : -m) + 7.f;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; i += 2) {
+      const float x = s[i >> 4][i & 15], y = s[i >> 4][(i & 15) + 1];
+      const prm_h2 e = {(half_t)__builtin_amdgcn_exp2f(__builtin_fmaf(x, scale2, off)),
+                        (half_t)__builtin_amdgcn_exp2f(__builtin_fmaf(y, scale2, off))};
+      sum = __builtin_amdgcn_fdot2(e, prm_h2{(half_t)1, (half_t)1}, sum, false);
+      w[i >> 3][i & 7] = e[0];
+      w[i >> 3][(i & 7) + 1] = e[1];
+    }
+    return sum;
+  };
+  // m is the largest score of the tiles up to the one that set it.  While the weights of a tile stay in range (the largest below
+  // 2^9 times that score's, or the sum would not be), it need not follow; if a row's do not, or it has seen nothing so far, it
+  // does, and what has been summed is scaled.  So most tiles need no maximum and no exchange between lanes.
+  auto weights = [&](int t) __attribute__((always_inline)) {
+    hide(t, s);
+    float sum = weigh();
+    if (!__all(sum <= 65536.f && m > -INFINITY)) {
+      float mx = s[0][0];
+#pragma unroll
+      for (int i = 1; i < 32; ++i) mx = fmaxf(mx, s[i >> 4][i & 15]);
+      mx = fmaxf(fmaxf(mx, __shfl_xor(mx, 32, AF_WAVE)) * scale2, m);
       const float corr = mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mx);
       m = mx;
       l *= corr;
 #pragma unroll
       for (int d = 0; d < DB; ++d) o[d] *= corr;
+      sum = weigh();
     }
-    // Weights times 2^15 (in the range of fp16), each to the nearest of its 11 bits: one more rounding of the size of the
-    // result's own, and independent from key to key.
-    const float off = (m == -INFINITY ? 0.f : -m) + 15.f;
-    half8 w[4];
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][i], scale2, off));
-        l += e;
-        w[kb * 2 + (i >> 3)][i & 7] = (half_t)e;
-      }
+    l += sum;
     __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int d = 0; d < DB; d += 2) {
-      values(v1, d + 1);
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int s4 = 0; s4 < 4; ++s4) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v0[s4], w[s4], o[d], 0, 0, 0);
-      __builtin_amdgcn_sched_barrier(0);
-      if (d + 2 < DB) values(v0, d + 2);
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int s4 = 0; s4 < 4; ++s4) o[d + 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v1[s4], w[s4], o[d + 1], 0, 0, 0);
-      __builtin_amdgcn_sched_barrier(0);
-    }
   };
-  // every wave's loads are in LDS (the barrier alone does not wait for loads that go there directly)
-  auto landed = [&]() __attribute__((always_inline)) {
-    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
-    __syncthreads();
+  auto wait_loads = [&]() __attribute__((always_inline)) {  // vmcnt(0)
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0F70);
+    turn_page();
+  };
+  auto sync = []() __attribute__((always_inline)) {  // lgkmcnt(0) and the barrier: loads stay in flight over it
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
   };
 
-  page_of(0);
-  fetch(0, s_k0, s_v0, s_bad[0]);
-  page_of(1);
-  for (int t = 0; t < tl.n; t += 2) {
-    landed();
-    if (t + 1 < tl.n) {
-      fetch(t + 1, s_k1, s_v1, s_bad[1]);
-      page_of(t + 2);
-    }
-    compute(t, s_k0, s_v0, s_bad[0]);
+  // Step t: products (values of t - 1, scores of t), then weights of t.  Keys of t and values of t - 1 are read in one step; the
+  // next ones, keys of t + 1 and values of t, are fetched meanwhile to the other buffers, which the step before has read.
+  // A barrier alone does not wait for loads that go to LDS directly.
+  auto step = [&](auto first, int t, half_t* k_now, half_t* k_next, half_t* v_before, half_t* v_now) __attribute__((always_inline)) {
+    __builtin_amdgcn_s_setprio(1);  // of the two waves of a SIMD, the one with products goes first
+    products(first, k_now, v_before, [&](int d) __attribute__((always_inline)) {
+      constexpr int PER = (2 * NI + DB - 1) / DB;
+#pragma unroll
+      for (int i = d * PER; i < (d + 1) * PER && i < 2 * NI; ++i) {
+        if (i < NI)
+          fetch(v.v + page_v, t, v_now, i, false);
+        else
+          fetch(v.k + page_k, t + 1, k_next, i - NI, true);
+      }
+      if (d == DB - 1) id_next = page_of(t + 2);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    __builtin_amdgcn_s_setprio(0);
+    if (t < tl.n) weights(t);
+    wait_loads();
+    sync();
+  };
+  if (tid == 0) s_gone = 0;
+  sync();
+  page_k = 0;
+  id_next = page_of(0);
+  turn_page();
+#pragma unroll
+  for (int i = 0; i < NI; ++i) fetch(v.k + page_k, 0, s_k0, i, true);
+  id_next = page_of(1);
+  wait_loads();
+  sync();
+  step(std::true_type{}, 0, s_k0, s_k1, s_v1, s_v0);
+  for (int t = 1;; t += 2) {
+    step(std::false_type{}, t, s_k1, s_k0, s_v0, s_v1);
+    if (t >= tl.n) break;
+    step(std::false_type{}, t + 1, s_k0, s_k1, s_v1, s_v0);
     if (t + 1 >= tl.n) break;
-    landed();
-    if (t + 2 < tl.n) {
-      fetch(t + 2, s_k0, s_v0, s_bad[0]);
-      page_of(t + 3);
-    }
-    compute(t + 1, s_k1, s_v1, s_bad[1]);
   }
 
   if (r0 + wave * 32 > r1) return;
@@ -260,15 +332,15 @@ __global__ __launch_bounds__(PRM_THREADS, 2) void paged_prompt_kernel(PagedAttnP
 
 int af_launch_paged_prompt(af_ctx* ctx, const PagedAttnParams& a, int head_dim, int short_q) {
   // as many workgroups as any division of the rows among the sequences can need
-  const long long rep = a.n_heads / a.v.n_kv, rows = (long long)a.v.n_rows * rep;
-  const long long longer = a.v.n_rows / (short_q + 1), seqs = a.v.n_seqs < longer ? a.v.n_seqs : longer;
-  const long long wgs = (rows / PRM_ROWS + seqs) * a.v.n_kv;
+  const long long rows = (long long)a.v.n_rows * (a.n_heads / a.v.n_kv), longer = a.v.n_rows / (short_q + 1);
+  const long long wgs = (rows / PRM_ROWS + (a.v.n_seqs < longer ? a.v.n_seqs : longer)) * a.v.n_kv;
   if (wgs > 0x7FFFFFFF) return AF_EINVAL;
   if (wgs == 0) return AF_OK;
+  const dim3 grid((unsigned)wgs), threads(PRM_WAVES * AF_WAVE);
   if (head_dim == 128)
-    hipLaunchKernelGGL(paged_prompt_kernel<128>, dim3((unsigned)wgs), dim3(PRM_THREADS), 0, ctx->stream, a, short_q);
+    hipLaunchKernelGGL(paged_prompt_kernel<128>, grid, threads, 0, ctx->stream, a, short_q);
   else
-    hipLaunchKernelGGL(paged_prompt_kernel<64>, dim3((unsigned)wgs), dim3(PRM_THREADS), 0, ctx->stream, a, short_q);
+    hipLaunchKernelGGL(paged_prompt_kernel<64>, grid, threads, 0, ctx->stream, a, short_q);
   AF_LAUNCH_CHECK();
   return AF_OK;
 }
