@@ -12,6 +12,9 @@
 #define SPL_STEP 32                      // keys of a wave at a time
 #define SPL_TILE (SPL_WAVES * SPL_STEP)  // keys of a workgroup at a time
 #define SPL_ROWS 16                      // rows (query heads x tokens that share a key head) of a workgroup
+#define SPL_RW (SPL_ROWS / SPL_WAVES)    // of them a wave's, in the sums
+#define SPL_JOIN 16                      // partial results that are joined at once
+#define SPL_MAX_WGS 1024                 // workgroups: SPL_JOIN sets of them, at most 64, are joined by one wave
 
 typedef float spl_f4 __attribute__((ext_vector_type(4)));
 typedef half_t spl_h2 __attribute__((ext_vector_type(2)));
@@ -19,7 +22,7 @@ typedef half_t spl_h2 __attribute__((ext_vector_type(2)));
 struct PagedSplitParams {
   PagedAttnParams a;
   float* part;       // [2 gridDim.x][slot_rows][HD + 2]
-  int* tickets;      // one per workgroup, zero between launches
+  int* tickets;      // two per workgroup, zero between launches
   int slot_rows;     // most rows of a group
   int short_q;       // sequences with more new tokens are the other kernel's
 };
@@ -233,71 +236,121 @@ __global__ __launch_bounds__(SPL_THREADS, 2) void paged_split_kernel(PagedSplitP
       else if (d < HD)
         *reinterpret_cast<half2v*>(p.a.out + (size_t)(seq.row0 + ta) * p.a.out_stride + (size_t)ha * HD + d) = half2v{(half_t)o0, (half_t)o1};
     };
-    float* slot = p.part + (size_t)(2 * blockIdx.x + (start > u0 ? 1 : 0)) * p.slot_rows * (HD + 2);
+    // partial result of this group's piece in workgroup w: [rows][maximum, sum, values]
+    auto slot = [&](int w) __attribute__((always_inline)) {
+      return p.part + (size_t)(2 * w + (start > (u64)w * share ? 1 : 0)) * p.slot_rows * (HD + 2);
+    };
     const int d = min(lane * 2, HD - 2);
-    for (int rr = wave; rr < rows; rr += SPL_WAVES) {
-      float M = -INFINITY, L = 0.f, v0 = 0.f, v1 = 0.f;
+    float M[SPL_RW], L[SPL_RW], v0[SPL_RW], v1[SPL_RW];  // of rows wave, wave + 4, ...
+    auto put = [&](float* to) __attribute__((always_inline)) {
 #pragma unroll
-      for (int w = 0; w < SPL_WAVES; ++w) M = fmaxf(M, s_ml[w][rr].x);
-      const float safe = M == -INFINITY ? 0.f : M;
+      for (int i = 0; i < SPL_RW; ++i)
+        if (wave + i * SPL_WAVES < rows) {
+          float* at = to + (wave + i * SPL_WAVES) * (HD + 2);
+          if (lane * 2 < HD) af_store_agent2(at + 2 + d, v0[i], v1[i]);
+          if (lane == 0) af_store_agent2(at, M[i], L[i]);
+        }
+    };
+    // The sum of `cnt` partial results, at from(i): lane i has the maximum and the sum of the i-th.  They come from other XCDs, so
+    // all rows' first sixteen are requested together.
+    auto join = [&](int cnt, auto&& from) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < SPL_RW; i += 2) {
+        if (wave + i * SPL_WAVES >= rows) continue;
+        const bool two = wave + (i + 1) * SPL_WAVES < rows;
+        const int ra = (wave + i * SPL_WAVES) * (HD + 2), rb = ra + SPL_WAVES * (HD + 2);
+        const float* mine = from(min(lane, cnt - 1));
+        af_float2 ml[2] = {af_load_agent2(mine + ra), af_float2{0.f, 0.f}};
+        if (two) ml[1] = af_load_agent2(mine + rb);
+        float f[2];
+        for (int c0 = 0; c0 < cnt; c0 += SPL_JOIN) {
+          af_float2 av[2][SPL_JOIN];
+#pragma unroll
+          for (int e = 0; e < SPL_JOIN; ++e) {
+            const float* at = from(min(c0 + e, cnt - 1)) + 2 + d;
+            av[0][e] = af_load_agent2(at + ra);
+            if (two) av[1][e] = af_load_agent2(at + rb);
+          }
+          if (c0 == 0) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              if (k && !two) continue;
+              float mx = lane < cnt ? ml[k][0] : -INFINITY;
+#pragma unroll
+              for (int off = 32; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor(mx, off, AF_WAVE));
+              f[k] = lane < cnt ? __builtin_amdgcn_exp2f(ml[k][0] - (mx == -INFINITY ? 0.f : mx)) : 0.f;
+              M[i + k] = mx;
+              L[i + k] = af_wave_sum(lane < cnt ? f[k] * ml[k][1] : 0.f);
+              v0[i + k] = v1[i + k] = 0.f;
+            }
+          }
+#pragma unroll
+          for (int e = 0; e < SPL_JOIN; ++e)
+            if (c0 + e < cnt) {
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                if (k && !two) continue;
+                const float w = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f[k]), c0 + e));
+                v0[i + k] += w * av[k][e][0];
+                v1[i + k] += w * av[k][e][1];
+              }
+            }
+        }
+      }
+    };
+    // last of `cnt` workgroups at ticket t
+    auto last_of = [&](int cnt, int t) __attribute__((always_inline)) {
+      af_stores_done();
+      __syncthreads();
+      if (tid == 0) {
+        s_last = af_ticket_take(&p.tickets[af_ticket_of(t)]) == cnt - 1;
+        if (s_last) af_ticket_reset(&p.tickets[af_ticket_of(t)]);
+      }
+      __syncthreads();
+      return s_last != 0;
+    };
+#pragma unroll
+    for (int i = 0; i < SPL_RW; ++i) {
+      const int rr = wave + i * SPL_WAVES;
+      if (rr >= rows) break;
+      M[i] = -INFINITY;
+      L[i] = v0[i] = v1[i] = 0.f;
+#pragma unroll
+      for (int w = 0; w < SPL_WAVES; ++w) M[i] = fmaxf(M[i], s_ml[w][rr].x);
+      const float safe = M[i] == -INFINITY ? 0.f : M[i];
 #pragma unroll
       for (int w = 0; w < SPL_WAVES; ++w) {
         const float f = __builtin_amdgcn_exp2f(s_ml[w][rr].x - safe);
-        L += f * s_ml[w][rr].y;
-        v0 += f * s_acc[w][rr][d];
-        v1 += f * s_acc[w][rr][d + 1];
-      }
-      if (whole) {
-        store(rr, v0, v1, L);
-      } else {
-        float* to = slot + rr * (HD + 2);
-        if (lane * 2 < HD) af_store_agent2(to + 2 + d, v0, v1);
-        if (lane == 0) af_store_agent2(to, M, L);
+        L[i] += f * s_ml[w][rr].y;
+        v0[i] += f * s_acc[w][rr][d];
+        v1[i] += f * s_acc[w][rr][d + 1];
       }
     }
+    bool done = whole;
     if (!whole) {
+      // Workgroups w0 .. w1 have the group's pieces.  Sixteen neighbours join theirs, and where there are more of them, the
+      // sixteens' sums are joined after that: a single workgroup would go through 64 pieces of eight rows for 17 us.
       const int w0 = (int)(start / share), w1 = (int)((start + (u64)tiles - 1) / share);
-      af_stores_done();
-      __syncthreads();
-      if (tid == 0) s_last = af_ticket_take(&p.tickets[af_ticket_of(w0)]) == w1 - w0;
-      __syncthreads();
-      if (s_last) {
-        for (int rr = wave; rr < rows; rr += SPL_WAVES) {
-          float M = -INFINITY, L = 0.f, v0 = 0.f, v1 = 0.f;
-          for (int c0 = w0; c0 <= w1; c0 += AF_WAVE) {  // lane i has the maximum and the sum of workgroup c0 + i
-            const int cnt = min(AF_WAVE, w1 - c0 + 1);
-            auto from = [&](int i) __attribute__((always_inline)) {
-              const int w = c0 + min(i, cnt - 1);
-              return p.part + ((size_t)(2 * w + (start > (u64)w * share ? 1 : 0)) * p.slot_rows + rr) * (HD + 2);
-            };
-            const af_float2 ml = af_load_agent2(from(lane));
-            float mx = lane < cnt ? ml[0] : -INFINITY;
-#pragma unroll
-            for (int off = 32; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor(mx, off, AF_WAVE));
-            mx = fmaxf(mx, M);
-            const float safe = mx == -INFINITY ? 0.f : mx, corr = __builtin_amdgcn_exp2f(M - safe);
-            const float f = lane < cnt ? __builtin_amdgcn_exp2f(ml[0] - safe) : 0.f;
-            M = mx;
-            L = L * corr + af_wave_sum(lane < cnt ? f * ml[1] : 0.f);
-            v0 *= corr;
-            v1 *= corr;
-            for (int i0 = 0; i0 < cnt; i0 += 16) {
-              af_float2 av[16];
-#pragma unroll
-              for (int e = 0; e < 16; ++e) av[e] = af_load_agent2(from(i0 + e) + 2 + d);
-#pragma unroll
-              for (int e = 0; e < 16; ++e)
-                if (i0 + e < cnt) {
-                  const float w = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), i0 + e));
-                  v0 += w * av[e][0];
-                  v1 += w * av[e][1];
-                }
-            }
-          }
-          store(rr, v0, v1, L);
+      const int first = w0 + ((int)blockIdx.x - w0) / SPL_JOIN * SPL_JOIN, cnt = min(SPL_JOIN, w1 - first + 1);
+      const int sets = (w1 - w0) / SPL_JOIN + 1;
+      done = true;
+      put(slot(blockIdx.x));
+      if (cnt > 1) {  // alone, it may be the first of another group: the ticket is that one's
+        done = last_of(cnt, first);
+        if (done) {
+          join(cnt, [&](int i) __attribute__((always_inline)) { return slot(first + i); });
+          if (sets > 1) put(slot(first));
         }
-        if (tid == 0) af_ticket_reset(&p.tickets[af_ticket_of(w0)]);
       }
+      if (done && sets > 1) {
+        done = last_of(sets, SPL_MAX_WGS + w0);
+        if (done) join(sets, [&](int i) __attribute__((always_inline)) { return slot(w0 + i * SPL_JOIN); });
+      }
+    }
+    if (done) {
+#pragma unroll
+      for (int i = 0; i < SPL_RW; ++i)
+        if (wave + i * SPL_WAVES < rows) store(wave + i * SPL_WAVES, v0[i], v1[i], L[i]);
     }
     u += (u64)(t1 - t0);
     if (u < u1) __syncthreads();  // the sums in LDS are read; the next stretch writes them
@@ -318,7 +371,7 @@ static int launch_attention(af_ctx* ctx, const PagedAttnParams& a) {
   size_t wgs = 2 * (size_t)ctx->n_cu;
   const size_t fit = floats / ((size_t)2 * slot_rows * (HD + 2));
   if (wgs > fit) wgs = fit;
-  if (wgs > AF_TICKET_ATTN) wgs = AF_TICKET_ATTN;  // as many tickets
+  if (wgs > SPL_MAX_WGS) wgs = SPL_MAX_WGS;
   if (wgs < 1) return AF_EWORKSPACE;
   const size_t lds = ((size_t)a.v.n_seqs + 1) * sizeof(unsigned long long) + (size_t)a.v.n_seqs * sizeof(PagedSeq);
   hipLaunchKernelGGL(paged_split_kernel<HD>, dim3((unsigned)wgs), dim3(SPL_THREADS), lds, ctx->stream, p);
