@@ -10,7 +10,7 @@ ROOT = os.path.dirname(PKG_DIR)
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libactiveflow.so")
 SOURCES = ["api.hip", "select.hip", "gemv_f16.hip", "gemv_q4.hip", "union.hip", "attention.hip", "layer.hip", "batch_layer.hip", "calib.hip", "planner.hip",
-           "paged_append.hip", "paged_attn.hip", "paged_prompt.hip"]
+           "paged_append.hip", "paged_attn.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950",

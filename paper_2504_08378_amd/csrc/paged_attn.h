@@ -72,6 +72,3 @@ __device__ __forceinline__ void paged_row(const PagedAttnParams& p, int b, int r
   }
   if (g == 0) *reinterpret_cast<half8*>(p.out + (size_t)row * p.out_stride + (size_t)h * HD + c0) = o;
 }
-
-// Sequences with more than short_q new tokens, many rows at a time (paged_prompt.hip).
-int af_launch_paged_prompt(af_ctx* ctx, const PagedAttnParams& a, int head_dim, int short_q);

@@ -17,8 +17,7 @@
 // loads between the products, with reads that the compiler could not tell from the loads' buffers (it waited for them) 667;
 // this form 573.  Eight waves on one pair of tiles, half of them a phase behind the others, 573; without the waves' priorities
 // 587.
-#include <math.h>
-
+#pragma once
 #include <type_traits>
 
 #include "paged_attn.h"
@@ -33,25 +32,26 @@ typedef __fp16 prm_fp16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) void prm_lds;
 typedef __attribute__((address_space(1))) const void prm_glb;
 
+// s_k0 .. s_v1: LDS of PRM_TILE * HD elements each, objects of their own.
 template <int HD>
-__global__ __launch_bounds__(PRM_WAVES * AF_WAVE, 2) void paged_prompt_kernel(PagedAttnParams p, int short_q) {
+__device__ __forceinline__ void paged_prompt_body(const PagedAttnParams& p, const int short_q, const unsigned wg, half_t* s_k0,
+                                                  half_t* s_k1, half_t* s_v0, half_t* s_v1) {
   constexpr int KS = HD / 16;        // contraction steps of the scores
   constexpr int DB = HD / 32;        // blocks of 32 dimensions
   constexpr int CH = HD / 8;         // 16-byte pieces of a row
   constexpr int RPI = AF_WAVE / CH;  // rows of a load instruction
   constexpr int KEYS = PRM_TILE / PRM_WAVES;  // keys of a tile that a wave loads
   constexpr int NI = KEYS / RPI;          // in so many instructions
-  __shared__ __align__(16) half_t s_k0[PRM_TILE * HD], s_k1[PRM_TILE * HD], s_v0[PRM_TILE * HD], s_v1[PRM_TILE * HD];
   __shared__ int s_gone;  // a page of this workgroup does not exist
 
   const PagedView& v = p.v;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 31, h = lane >> 5;
   const int rep = p.n_heads / v.n_kv, window = p.window, n_sink = p.n_sink;
-  const int kvh = (int)(blockIdx.x % (unsigned)v.n_kv);
+  const int kvh = (int)(wg % (unsigned)v.n_kv);
 
   // which sequence, and which of its 128 rows: the last ones first, they see most
-  int b = -1, tile = (int)(blockIdx.x / (unsigned)v.n_kv);
+  int b = -1, tile = (int)(wg / (unsigned)v.n_kv);
   PagedSeq seq{0, 0, 0};
   for (int b0 = 0; b0 < v.n_seqs && b < 0; b0 += AF_WAVE) {
     PagedSeq s{0, 0, 0};
@@ -328,19 +328,4 @@ __global__ __launch_bounds__(PRM_WAVES * AF_WAVE, 2) void paged_prompt_kernel(Pa
     const int rr = r0 + wave * 32 + k, tt = rr / rep;
     paged_row<HD>(p, b, seq.row0 + tt, p0 + tt, kvh * rep + (rr - tt * rep));
   }
-}
-
-int af_launch_paged_prompt(af_ctx* ctx, const PagedAttnParams& a, int head_dim, int short_q) {
-  // as many workgroups as any division of the rows among the sequences can need
-  const long long rows = (long long)a.v.n_rows * (a.n_heads / a.v.n_kv), longer = a.v.n_rows / (short_q + 1);
-  const long long wgs = (rows / PRM_ROWS + (a.v.n_seqs < longer ? a.v.n_seqs : longer)) * a.v.n_kv;
-  if (wgs > 0x7FFFFFFF) return AF_EINVAL;
-  if (wgs == 0) return AF_OK;
-  const dim3 grid((unsigned)wgs), threads(PRM_WAVES * AF_WAVE);
-  if (head_dim == 128)
-    hipLaunchKernelGGL(paged_prompt_kernel<128>, grid, threads, 0, ctx->stream, a, short_q);
-  else
-    hipLaunchKernelGGL(paged_prompt_kernel<64>, grid, threads, 0, ctx->stream, a, short_q);
-  AF_LAUNCH_CHECK();
-  return AF_OK;
 }

@@ -185,6 +185,18 @@ def test_a_few_new_tokens(ctx, new):
 
 
 @pytest.mark.parametrize("single", [True, False])
+def test_as_many_sequences_as_there_may_be(ctx, single):
+    heads, kv, hd = 2, 1, 64
+    rng = np.random.default_rng(3)
+    lens = [(int(n), 1 if single else int(min(n, q))) for n, q in zip(rng.integers(1, 40, 1024), rng.choice([0, 1, 2, 12], 1024))]
+    lens[700] = (2500, 1 if single else 300)
+    bt = Batch(lens, kv, hd, 16, seed=3, single=single)
+    q, got = run(ctx, bt, heads)
+    check(got, attend(bt, q, heads), heads, hd, weights16=not single)
+    run_append(ctx, bt, heads)
+
+
+@pytest.mark.parametrize("single", [True, False])
 def test_strides_scale_and_spaced_pages(ctx, single):
     heads, kv, hd = 6, 3, 64
     lens = [(200, 1), (33, 1)] if single else [(90, 80), (20, 20), (400, 2)]
@@ -324,20 +336,21 @@ def run_append(ctx, bt, heads, in_place=False, no_q=False, pad=0, theta=10000.0,
     ctx.synchronize()
     assert ctx.last_device_error() == err
     K, V = bt.K.copy(), bt.V.copy()
+    where = {r: (b, p) for r, b, p in bt.tokens()}
+    Kg, qg = to_host(bt.Kd), None if no_q else to_host(q_out)
     for row, (x, mag) in append_ref(bt, qkv, heads, theta, gains, eps, pos).items():
-        b, place = next((b, p) for r, b, p in bt.tokens() if r == row)
+        b, place = where[row]
         at = bt.table[b, place // bt.page], slice(None), place % bt.page
         # one rounding, and fp32 on the way: angle (2^-25 of a turn), norm, products
         tol = 2.0 ** -11 * np.abs(x) + 2.0 ** -25 + 2.0 ** -20 * mag
-        got = to_host(bt.Kd)[at].astype(np.float64)
-        assert np.all(np.abs(got - x[heads:]) <= tol[heads:]), row
-        K[at] = to_host(bt.Kd)[at]
+        assert np.all(np.abs(Kg[at].astype(np.float64) - x[heads:]) <= tol[heads:]), row
+        K[at] = Kg[at]
         V[at] = qkv[row].reshape(-1, bt.hd)[heads + bt.kv:]
         if not no_q:
-            got = to_host(q_out)[row].astype(np.float64).reshape(heads, bt.hd)
+            got = qg[row].astype(np.float64).reshape(heads, bt.hd)
             assert np.all(np.abs(got - x[:heads]) <= tol[:heads]), row
     # and nothing else has changed
-    assert np.array_equal(to_host(bt.Kd).view(np.uint16), K.view(np.uint16))
+    assert np.array_equal(Kg.view(np.uint16), K.view(np.uint16))
     assert np.array_equal(to_host(bt.Vd).view(np.uint16), V.view(np.uint16))
     if not no_q:
         rows = {r for r, _, _ in bt.tokens()}
