@@ -233,14 +233,14 @@ class PagedCache:
         for t, name in ((k_pages, "k_pages"), (v_pages, "v_pages")):
             if not t.is_cuda or t.dtype != torch.float16 or t.dim() != 4:
                 raise TypeError(f"{name} must be a CUDA tensor of fp16 with four dimensions")
-            n, kv, page, hd = t.shape
-            if t.shape != k_pages.shape or t.stride()[1:] != (page * hd, hd, 1) or \
+            n = t.shape[0]
+            if n == 0 or t.shape != k_pages.shape or not t[0].is_contiguous() or \
                     (n > 1 and t.stride(0) != k_pages.stride(0)):
                 raise TypeError(f"{name} must be contiguous inside a page, and shaped and spaced as k_pages")
         if k_pages.device != v_pages.device:
             raise TypeError("k_pages and v_pages must be on one device")
         n, kv, page, hd = k_pages.shape
-        self.k_pages, self.v_pages, self.device = k_pages, v_pages, k_pages.device
+        self.k_pages, self.v_pages, self.index = k_pages, v_pages, k_pages.get_device()
         self.n_kv_heads, self.head_dim = kv, hd
         self.struct = PagedCacheStruct(k_pages.data_ptr(), v_pages.data_ptr(),
                                        k_pages.stride(0) if n > 1 else kv * page * hd, n, page, kv, hd)
@@ -261,8 +261,8 @@ class PagedBatch:
         elif q_start.numel() != n_seqs + 1 or n_rows is None:
             raise TypeError("q_start must have n_seqs + 1 entries, and n_rows be given with it")
         self.page_table, self.kv_len, self.q_start, self.n_rows = page_table, kv_len, q_start, int(n_rows)
-        self.n_seqs, self.device = n_seqs, kv_len.device
-        if page_table.device != self.device or (q_start is not None and q_start.device != self.device):
+        self.n_seqs, self.index = n_seqs, kv_len.get_device()
+        if page_table.get_device() != self.index or (q_start is not None and q_start.get_device() != self.index):
             raise TypeError("the tensors of a batch must be on one device")
         self.struct = PagedBatchStruct(
             n_seqs, page_table.shape[1], self.n_rows, int(self.n_rows if max_q_len is None else max_q_len),
@@ -548,22 +548,22 @@ class Context:
             C.byref(sets) if sets is not None else None, C.byref(route)), "af_decode_moe_layer")
 
     # ---- paged cache -----------------------------------------------------------------
-    def _paged_rows(self, t, batch: PagedBatch, width: int, name: str):
+    def _paged_rows(self, t, n_rows: int, width: int, name: str):
         """(address, row stride) of a token tensor [n_rows][...] whose rows are contiguous."""
-        if t.dtype != torch.float16 or t.device != self.device:
+        if t.dtype is not torch.float16 or t.get_device() != self.device.index:
             raise TypeError(f"{name} must be fp16 on the context's device")
-        n = t.shape[0]
-        if n < batch.n_rows or t.numel() != n * width:
-            raise TypeError(f"{name} must have at least {batch.n_rows} rows of {width}")
+        shape, stride = t.shape, t.stride()
+        n = shape[0]
+        if n < n_rows or t.numel() != n * width:
+            raise TypeError(f"{name} must have at least {n_rows} rows of {width}")
         if n == 0:
             return None, width
-        inner = t.stride()[1:]
-        if inner != (1,) and (t.dim() != 3 or inner != (t.shape[2], 1)):
+        if not (len(shape) == 2 and stride[1] == 1 or t[0].is_contiguous()):
             raise TypeError(f"{name} must be contiguous inside a row")
-        return t.data_ptr(), t.stride(0) if n > 1 else width
+        return t.data_ptr(), stride[0] if n > 1 else width
 
     def _paged_check(self, cache: PagedCache, batch: PagedBatch):
-        if cache.device != self.device or batch.device != self.device:
+        if cache.index != self.device.index or batch.index != self.device.index:
             raise TypeError("cache and batch must be on the context's device")
 
     def paged_append(self, cache: PagedCache, batch: PagedBatch, qkv, q_out, n_heads: int, rope_theta: float = 10000.0,
@@ -572,8 +572,8 @@ class Context:
         [n_rows][n_heads head_dim] (None: not stored; the q columns of qkv will do) receives the rotated queries."""
         self._paged_check(cache, batch)
         hd = cache.head_dim
-        src, src_ld = self._paged_rows(qkv, batch, (n_heads + 2 * cache.n_kv_heads) * hd, "qkv")
-        dst, dst_ld = (None, 0) if q_out is None else self._paged_rows(q_out, batch, n_heads * hd, "q_out")
+        src, src_ld = self._paged_rows(qkv, batch.n_rows, (n_heads + 2 * cache.n_kv_heads) * hd, "qkv")
+        dst, dst_ld = (None, 0) if q_out is None else self._paged_rows(q_out, batch.n_rows, n_heads * hd, "q_out")
         for t, name in ((q_gain, "q_gain"), (k_gain, "k_gain")):
             if t is not None and (t.numel() != hd or t.device != self.device):
                 raise TypeError(f"{name} must have {hd} entries on the context's device")
@@ -589,8 +589,8 @@ class Context:
         """Attention of the batch's new tokens over their pages: q, out [n_rows][n_heads head_dim]."""
         self._paged_check(cache, batch)
         width = n_heads * cache.head_dim
-        src, src_ld = self._paged_rows(q, batch, width, "q")
-        dst, dst_ld = self._paged_rows(out, batch, width, "out")
+        src, src_ld = self._paged_rows(q, batch.n_rows, width, "q")
+        dst, dst_ld = self._paged_rows(out, batch.n_rows, width, "out")
         _check(lib().af_paged_attention(self._h, cache._ref, batch._ref, n_heads, scale, window, n_sink, src, src_ld,
                                         dst, dst_ld), "af_paged_attention")
         return out

@@ -68,6 +68,10 @@ struct af_ctx {
   // launch-shape overrides for tuning sweeps (af_set_option; 0 = the built-in heuristic)
   int tune_lx, tune_nw, tune_split, tune_wgs, moe_router_kernel, tune_attn_splits, tune_early_rows;
   int layer_kernel_state; // 0 not probed yet, 1 usable, -1 not usable on this device
+  // af_paged_append: angles per position, in turns, of the last rope_theta and head width (0: none yet)
+  float rope_theta;
+  int rope_dim;
+  double rope_turns[64];
 };
 
 // Slot of the next layer kernel's time stamps (null: profiling off or slots used up).

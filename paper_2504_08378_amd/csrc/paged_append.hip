@@ -9,14 +9,18 @@
 //
 // Bound by memory: the rows are read and written once.  A lane has eight neighbouring elements and the eight
 // half a head further, both sides of eight rotations in 16-byte pieces; so a head is 8 lanes (4 at width 64),
-// its norm three exchanges inside them.  The angles of a token are formed once, by 64 lanes side by side,
-// and go through LDS to the lanes of all heads.
+// its norm three exchanges inside them.  A wave works for itself: it has one token (or, where there are few tokens, a
+// quarter of one's heads), requests its first heads before it looks for the token's sequence and page, forms the
+// token's angles with a lane for each, and hands them to the lanes of all heads through LDS.
 #include <math.h>
+#include <string.h>
 
 #include "paged.h"
 
 #define APP_THREADS 256
 #define APP_WAVES (APP_THREADS / AF_WAVE)
+
+#define APP_AHEAD 4  // heads of a lane that are requested together
 
 struct AppendParams {
   PagedView v;
@@ -35,96 +39,114 @@ template <int HD, int WPT>
 __global__ __launch_bounds__(APP_THREADS) void paged_append_kernel(AppendParams p) {
   constexpr int LPH = HD / 16;              // lanes of a head
   constexpr int HPW = AF_WAVE / LPH;        // heads of a wave at a time
-  constexpr int TOKENS = APP_WAVES / WPT;   // of a workgroup
-  __shared__ float s_cs[TOKENS][HD / 2], s_sn[TOKENS][HD / 2];
-  __shared__ int s_seq[TOKENS], s_at[TOKENS], s_page[TOKENS], s_pos[TOKENS];
+  __shared__ __align__(16) float s_cs[APP_WAVES][HD / 2], s_sn[APP_WAVES][HD / 2];
   const PagedView& v = p.v;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int first = blockIdx.x * TOKENS;
-  if (tid < TOKENS) s_seq[tid] = -1;
-  __syncthreads();
-  // the sequences of this workgroup's rows
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row = blockIdx.x * (APP_WAVES / WPT) + wave / WPT;
+  if (row >= v.n_rows) return;
+
+  const int i0 = lane % LPH * 8, heads = p.n_heads + 2 * v.n_kv;
+  const int h0 = wave % WPT * HPW + lane / LPH;  // the lane's first head; the next is WPT * HPW further
+  const half_t* src = p.qkv + (size_t)row * p.qkv_stride + i0;
+  half8 a[APP_AHEAD], b[APP_AHEAD];
+  auto fetch = [&](int h) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < APP_AHEAD; ++u) {
+      const size_t o = (size_t)min(h + u * WPT * HPW, heads - 1) * HD;
+      a[u] = af_load_once(reinterpret_cast<const half8*>(src + o));
+      b[u] = af_load_once(reinterpret_cast<const half8*>(src + o + HD / 2));
+    }
+  };
+  fetch(h0);
+
+  // the row's sequence; numbers that cannot be right are reported by whoever meets them, all by the first wave
+  int seq = row;
+  PagedSeq s{0, 0, 0};
   if (v.q_start) {
-    for (int b = tid; b < v.n_seqs; b += APP_THREADS) {
-      const PagedSeq s = paged_seq(v, b);
-      for (int t = max(s.row0, first); t < min(s.row0 + s.q_len, first + TOKENS); ++t) s_seq[t - first] = b;
+    seq = -1;
+    for (int b0 = 0; b0 < v.n_seqs && (seq < 0 || row == 0); b0 += AF_WAVE) {
+      PagedSeq c{0, 0, 0};
+      if (b0 + lane < v.n_seqs) c = paged_seq(v, b0 + lane);
+      const unsigned long long hit = __ballot(c.row0 <= row && row < c.row0 + c.q_len);
+      if (hit && seq < 0) {
+        const int l = __builtin_ctzll(hit);
+        seq = b0 + l;
+        s = PagedSeq{__builtin_amdgcn_readlane(c.row0, l), __builtin_amdgcn_readlane(c.q_len, l), __builtin_amdgcn_readlane(c.len, l)};
+      }
     }
-    __syncthreads();
-  } else if (tid < TOKENS && first + tid < v.n_rows) {
-    s_seq[tid] = first + tid;
+    if (seq < 0) return;
+  } else {
+    s = paged_seq(v, row);
   }
-  if (tid < TOKENS) {
-    const int b = s_seq[tid];
-    int at = -1, page = -1;
-    if (b >= 0) {
-      const PagedSeq s = paged_seq(v, b);
-      const int i = first + tid - s.row0;
-      if (i >= 0 && i < s.q_len) at = s.len - s.q_len + i;  // -1: no token (an empty sequence)
-      if (at >= 0) page = paged_page(v, b, at);
-    }
-    s_at[tid] = at;
-    s_page[tid] = page;
-    s_pos[tid] = at >= 0 && p.pos ? p.pos[first + tid] : at;
-  }
-  __syncthreads();
-  for (int e = tid; e < TOKENS * (HD / 2); e += APP_THREADS) {
-    const int t = e / (HD / 2), i = e % (HD / 2);
-    const double turns = (double)s_pos[t] * p.turns[i];
+  const int at = s.q_len > 0 ? s.len - s.q_len + row - s.row0 : -1;
+  if (at < 0) return;  // no token (an empty sequence, or one that cannot be right)
+  const int page = paged_page(v, seq, at);
+  if (page < 0) return;
+
+  const int pos = p.pos ? p.pos[row] : at;
+  if (lane < HD / 2) {
+    const double turns = (double)pos * p.turns[lane];
     float sn, cs;
     sincospif(2.0f * (float)(turns - rint(turns)), &sn, &cs);
-    s_cs[t][i] = cs;
-    s_sn[t][i] = sn;
+    s_cs[wave][lane] = cs;
+    s_sn[wave][lane] = sn;
   }
-  __syncthreads();
-
-  const int t = wave / WPT, row = first + t;
-  if (s_page[t] < 0) return;
-  const int lk = lane % LPH, i0 = lk * 8;
-  const half_t* src = p.qkv + (size_t)row * p.qkv_stride + i0;
-  const int heads = p.n_heads + 2 * v.n_kv;
-  for (int h = (wave % WPT) * HPW + lane / LPH; h < heads; h += WPT * HPW) {
-    half8 a = *reinterpret_cast<const half8*>(src + (size_t)h * HD);
-    half8 b = *reinterpret_cast<const half8*>(src + (size_t)h * HD + HD / 2);
-    half_t* dst;
-    if (h < p.n_heads)
-      dst = p.q_out ? p.q_out + (size_t)row * p.q_stride + (size_t)h * HD : nullptr;
-    else if (h < p.n_heads + v.n_kv)
-      dst = v.k + paged_offset(v, s_page[t], h - p.n_heads, s_at[t], HD);
-    else
-      dst = v.v + paged_offset(v, s_page[t], h - p.n_heads - v.n_kv, s_at[t], HD);
-    if (h < p.n_heads + v.n_kv) {
-      float x[8], y[8];
+  __builtin_amdgcn_wave_barrier();  // a wave's LDS accesses are done in order
+  float cs[8], sn[8];
 #pragma unroll
-      for (int c = 0; c < 8; ++c) {
-        x[c] = (float)a[c];
-        y[c] = (float)b[c];
-      }
-      const half_t* gain = h < p.n_heads ? p.q_gain : p.k_gain;
-      if (gain) {
-        float s = 0.f;
+  for (int c = 0; c < 8; ++c) {
+    cs[c] = s_cs[wave][i0 + c];
+    sn[c] = s_sn[wave][i0 + c];
+  }
+  half_t* const dk = v.k + paged_offset(v, page, 0, at, HD) + i0;
+  half_t* const dv = v.v + paged_offset(v, page, 0, at, HD) + i0;
+  half_t* const dq = p.q_out ? p.q_out + (size_t)row * p.q_stride + i0 : nullptr;
+  for (int h1 = h0;; h1 += APP_AHEAD * WPT * HPW) {
 #pragma unroll
-        for (int c = 0; c < 8; ++c) s += x[c] * x[c] + y[c] * y[c];
-#pragma unroll
-        for (int off = 1; off < LPH; off <<= 1) s += __shfl_xor(s, off, AF_WAVE);
-        const float r = 1.0f / sqrtf(s * (1.0f / HD) + p.eps);
-        const half8 ga = *reinterpret_cast<const half8*>(gain + i0), gb = *reinterpret_cast<const half8*>(gain + i0 + HD / 2);
+    for (int u = 0; u < APP_AHEAD; ++u) {
+      const int h = h1 + u * WPT * HPW;
+      if (h >= heads) continue;
+      half8 ra = a[u], rb = b[u];
+      half_t* dst = dq ? dq + (size_t)h * HD : nullptr;
+      if (h >= p.n_heads + v.n_kv)
+        dst = dv + ((size_t)(h - p.n_heads - v.n_kv) << v.page_shift) * HD;
+      else if (h >= p.n_heads)
+        dst = dk + ((size_t)(h - p.n_heads) << v.page_shift) * HD;
+      if (h < p.n_heads + v.n_kv) {
+        float x[8], y[8];
 #pragma unroll
         for (int c = 0; c < 8; ++c) {
-          x[c] = x[c] * r * (float)ga[c];
-          y[c] = y[c] * r * (float)gb[c];
+          x[c] = (float)ra[c];
+          y[c] = (float)rb[c];
+        }
+        const half_t* gain = h < p.n_heads ? p.q_gain : p.k_gain;
+        if (gain) {
+          float sum = 0.f;
+#pragma unroll
+          for (int c = 0; c < 8; ++c) sum += x[c] * x[c] + y[c] * y[c];
+#pragma unroll
+          for (int off = 1; off < LPH; off <<= 1) sum += __shfl_xor(sum, off, AF_WAVE);
+          const float r = 1.0f / sqrtf(sum * (1.0f / HD) + p.eps);
+          const half8 ga = *reinterpret_cast<const half8*>(gain + i0), gb = *reinterpret_cast<const half8*>(gain + i0 + HD / 2);
+#pragma unroll
+          for (int c = 0; c < 8; ++c) {
+            x[c] = x[c] * r * (float)ga[c];
+            y[c] = y[c] * r * (float)gb[c];
+          }
+        }
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          ra[c] = (half_t)__builtin_fmaf(x[c], cs[c], -(y[c] * sn[c]));
+          rb[c] = (half_t)__builtin_fmaf(y[c], cs[c], x[c] * sn[c]);
         }
       }
-#pragma unroll
-      for (int c = 0; c < 8; ++c) {
-        const float cs = s_cs[t][i0 + c], sn = s_sn[t][i0 + c];
-        a[c] = (half_t)__builtin_fmaf(x[c], cs, -(y[c] * sn));
-        b[c] = (half_t)__builtin_fmaf(y[c], cs, x[c] * sn);
+      if (dst) {
+        *reinterpret_cast<half8*>(dst) = ra;
+        *reinterpret_cast<half8*>(dst + HD / 2) = rb;
       }
     }
-    if (dst) {
-      *reinterpret_cast<half8*>(dst + i0) = a;
-      *reinterpret_cast<half8*>(dst + i0 + HD / 2) = b;
-    }
+    if (h1 - lane / LPH + APP_AHEAD * WPT * HPW >= heads) break;  // the same for the wave
+    fetch(h1 + APP_AHEAD * WPT * HPW);
   }
 }
 
@@ -200,8 +222,13 @@ extern "C" int af_paged_append(af_ctx* ctx, const af_paged_cache* cache, const a
   p.q_stride = q_out_stride;
   p.n_heads = n_heads;
   p.eps = eps;
-  for (int i = 0; i < hd / 2; ++i)
-    p.turns[i] = pow((double)rope_theta, -2.0 * (double)i / (double)hd) / 6.283185307179586476925286766559;
+  if (ctx->rope_theta != rope_theta || ctx->rope_dim != hd) {  // 64 powers take the host longer than the launch
+    for (int i = 0; i < hd / 2; ++i)
+      ctx->rope_turns[i] = pow((double)rope_theta, -2.0 * (double)i / (double)hd) / 6.283185307179586476925286766559;
+    ctx->rope_theta = rope_theta;
+    ctx->rope_dim = hd;
+  }
+  memcpy(p.turns, ctx->rope_turns, sizeof(p.turns));
   const int rows = batch->n_rows;
   const bool few = rows < 4 * ctx->n_cu;
   const dim3 grid(few ? rows : (rows + APP_WAVES - 1) / APP_WAVES), threads(APP_THREADS);
