@@ -6,7 +6,6 @@
 #define SPL_THREADS 256
 #define SPL_WAVES (SPL_THREADS / AF_WAVE)
 #define SPL_STEP 32                      // keys of a wave at a time
-#define SPL_TILE (SPL_WAVES * SPL_STEP)  // keys of a workgroup at a time
 #define SPL_ROWS 16                      // rows (query heads x tokens that share a key head) of a workgroup
 #define SPL_RW (SPL_ROWS / SPL_WAVES)    // of them a wave's, in the sums
 #define SPL_JOIN 16                      // partial results that are joined at once
@@ -23,13 +22,15 @@ struct PagedSplitParams {
   int short_q;       // sequences with more new tokens are the other kernel's
 };
 
+PAGED_HD int paged_split_units(const PagedTiles& t) { return t.n > SPL_WAVES ? (t.n + SPL_WAVES - 1) / SPL_WAVES : 1; }
 static inline size_t paged_split_lds(int n_seqs) {
   return ((size_t)n_seqs + 1) * sizeof(unsigned long long) + (size_t)n_seqs * sizeof(PagedSeq);
 }
 
-// The work of the launch is a line of units, a tile of keys for one group of rows each, in the order sequence, key
-// head, group, tile; every workgroup takes an equal stretch of it.  A group whose tiles lie in several stretches
-// is joined by the workgroup that finishes last.
+// The work of the launch is a line of units, a step of each of the four waves for one group of rows, in the order sequence, key
+// head, group, key; every workgroup takes an equal stretch of it.  A group whose units lie in several stretches is joined by the
+// workgroup that finishes last.  (Stretches of single steps balance better under a window, 35.3 for 36.8 us, but cut more
+// groups and put short ones on single waves: eight sequences of up to 517 keys 15.6 for 10.4, 256 of up to 1500 106 for 95.)
 // wg of wgs workgroups; acc: LDS for a wave's sums each, [SPL_ROWS][HD + 4]; s_first: LDS of paged_split_lds() bytes.
 template <int HD>
 __device__ __forceinline__ void paged_split_body(const PagedSplitParams& p, const int wg, const int wgs,
@@ -58,8 +59,8 @@ __device__ __forceinline__ void paged_split_body(const PagedSplitParams& p, cons
     s_seq[b] = s;
     s_first[b] = mine;
     if (s.q_len > 0 && s.q_len <= p.short_q) {
-      const int tiles = max(1, paged_tiles<SPL_TILE>(s.len - s.q_len, s.len - 1, window, n_sink).n);
-      mine += (u64)((s.q_len * rep + SPL_ROWS - 1) / SPL_ROWS) * (unsigned)v.n_kv * (u64)tiles;
+      const int units = paged_split_units(paged_tiles<SPL_STEP>(s.len - s.q_len, s.len - 1, window, n_sink));
+      mine += (u64)((s.q_len * rep + SPL_ROWS - 1) / SPL_ROWS) * (unsigned)v.n_kv * (u64)units;
     }
   }
   u64 incl = mine;
@@ -76,7 +77,7 @@ __device__ __forceinline__ void paged_split_body(const PagedSplitParams& p, cons
     if (w < wave) before += s_sum[w];
     total += s_sum[w];
   }
-  const u64 share = total >> 32 ? (total + (unsigned)wgs - 1) / (unsigned)wgs : ((unsigned)total + wgs - 1) / (unsigned)wgs;
+  const u64 share = total >> 31 ? (total + (unsigned)wgs - 1) / (unsigned)wgs : ((unsigned)total + wgs - 1) / (unsigned)wgs;
   const u64 u0 = (u64)wg * share, u1 = min(u0 + share, total);
   if (u0 >= u1) return;
   for (int b = tid * per; b < min(tid * per + per, v.n_seqs); ++b) {
@@ -92,11 +93,11 @@ __device__ __forceinline__ void paged_split_body(const PagedSplitParams& p, cons
     while (u >= s_first[b + 1]) ++b;
     const PagedSeq seq = s_seq[b];
     const int p0 = seq.len - seq.q_len, p1 = seq.len - 1, rows_all = seq.q_len * rep, groups = (rows_all + SPL_ROWS - 1) / SPL_ROWS;
-    const PagedTiles tl = paged_tiles<SPL_TILE>(p0, p1, window, n_sink);
-    const int tiles = max(1, tl.n);
+    const PagedTiles tl = paged_tiles<SPL_STEP>(p0, p1, window, n_sink);
+    const int units = paged_split_units(tl);
     const u64 local = u - s_first[b];
-    const unsigned hg = local >> 32 ? (unsigned)(local / (unsigned)tiles) : (unsigned)local / (unsigned)tiles;
-    const int t0 = (int)(local - (u64)hg * (unsigned)tiles), t1 = (int)min((u64)tiles, t0 + (u1 - u));
+    const unsigned hg = local >> 32 ? (unsigned)(local / (unsigned)units) : (unsigned)local / (unsigned)units;
+    const int t0 = (int)(local - (u64)hg * (unsigned)units), t1 = (int)min((u64)units, t0 + (u1 - u));
     const int kvh = groups == 1 ? (int)hg : (int)(hg / (unsigned)groups), grp = (int)hg - kvh * groups;
     const int r0 = grp * SPL_ROWS, rows = min(SPL_ROWS, rows_all - r0);
 
@@ -109,14 +110,14 @@ __device__ __forceinline__ void paged_split_body(const PagedSplitParams& p, cons
       q[t] = *reinterpret_cast<const half8*>(p.a.q + (size_t)(seq.row0 + tok) * p.a.q_stride + (size_t)head * HD + t * 32 + g * 8);
 
     const int32_t* table = v.table + (size_t)b * v.table_stride;
-    const int mask = (1 << v.page_shift) - 1, last = seq.len - 1;
+    const int mask = (1 << v.page_shift) - 1, last = seq.len - 1, end = min(t1 * SPL_WAVES, tl.n);  // steps up to here
     int id[2];
     bool bad[2];
     half8 kr[2][TT];
     vrow vr[8];
     // pages of the two 16 keys of a step (what lies behind the sequence's end is read as its last row and masked)
     auto ids = [&](int t) __attribute__((always_inline)) {
-      const int k = paged_tile_start<SPL_TILE>(tl, min(t, t1 - 1)) + wave * SPL_STEP;
+      const int k = paged_tile_start<SPL_STEP>(tl, min(t, end - 1));
 #pragma unroll
       for (int i = 0; i < 2; ++i) id[i] = table[max(0, min(k + i * 16, last)) >> v.page_shift];
     };
@@ -143,74 +144,71 @@ __device__ __forceinline__ void paged_split_body(const PagedSplitParams& p, cons
     const spl_f4 zero4 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int c = 0; c < VC; ++c) acc[c] = zero4;
-    int t = t0;
-    int k0 = paged_tile_start<SPL_TILE>(tl, t) + wave * SPL_STEP;
+    int t = t0 * SPL_WAVES + wave, k0 = paged_tile_start<SPL_STEP>(tl, t);
     ids(t);
-    if (k0 <= last) fetch(k0);
-    ids(t + 1);
-    for (; t < t1; ++t) {
-      if (k0 <= last) {
-        // scores of keys k0 + 16 i + 4 g + e, row n
-        float sc[8];
+    if (t < end) fetch(k0);
+    ids(t + SPL_WAVES);
+    for (; t < end; t += SPL_WAVES) {
+      // scores of keys k0 + 16 i + 4 g + e, row n
+      float sc[8];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          spl_f4 d = zero4;
+      for (int i = 0; i < 2; ++i) {
+        spl_f4 d = zero4;
 #pragma unroll
-          for (int tt = 0; tt < TT; ++tt) d = __builtin_amdgcn_mfma_f32_16x16x32_f16(kr[i][tt], q[tt], d, 0, 0, 0);
+        for (int tt = 0; tt < TT; ++tt) d = __builtin_amdgcn_mfma_f32_16x16x32_f16(kr[i][tt], q[tt], d, 0, 0, 0);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) sc[i * 4 + e] = d[e] * p.a.scale2;
-        }
-        const bool inside = k0 + SPL_STEP - 1 <= p0 && (window <= 0 || k0 > p1 - window || k0 + SPL_STEP <= n_sink);
-        if (!inside || bad[0] || bad[1]) {
-          if (bad[0] || bad[1]) paged_report(v);
+        for (int e = 0; e < 4; ++e) sc[i * 4 + e] = d[e] * p.a.scale2;
+      }
+      const bool inside = k0 + SPL_STEP - 1 <= p0 && (window <= 0 || k0 > p1 - window || k0 + SPL_STEP <= n_sink);
+      if (!inside || bad[0] || bad[1]) {
+        if (bad[0] || bad[1]) paged_report(v);
 #pragma unroll
-          for (int j = 0; j < 8; ++j)
-            if (bad[j >> 2] || !paged_seen(k0 + (j >> 2) * 16 + g * 4 + (j & 3), place, window, n_sink)) sc[j] = -INFINITY;
-        }
-        float mx = sc[0];
+        for (int j = 0; j < 8; ++j)
+          if (bad[j >> 2] || !paged_seen(k0 + (j >> 2) * 16 + g * 4 + (j & 3), place, window, n_sink)) sc[j] = -INFINITY;
+      }
+      float mx = sc[0];
 #pragma unroll
-        for (int j = 1; j < 8; ++j) mx = fmaxf(mx, sc[j]);
-        mx = fmaxf(mx, __shfl_xor(mx, 16, AF_WAVE));
-        mx = fmaxf(mx, __shfl_xor(mx, 32, AF_WAVE));
-        mx = fmaxf(mx, m);
-        const float safe = mx == -INFINITY ? 0.f : mx;
-        if (__any(m != mx)) {
-          const float corr = __builtin_amdgcn_exp2f(m - safe);
-          l *= corr;
+      for (int j = 1; j < 8; ++j) mx = fmaxf(mx, sc[j]);
+      mx = fmaxf(mx, __shfl_xor(mx, 16, AF_WAVE));
+      mx = fmaxf(mx, __shfl_xor(mx, 32, AF_WAVE));
+      mx = fmaxf(mx, m);
+      const float safe = mx == -INFINITY ? 0.f : mx;
+      if (__any(m != mx)) {
+        const float corr = __builtin_amdgcn_exp2f(m - safe);
+        l *= corr;
 #pragma unroll
-          for (int c = 0; c < VC; ++c) acc[c] *= corr;
-        }
-        m = mx;
-        // weights times 2^15 (in the range of fp16) as a rounded value and a rest: 22 bits
-        u32x4 ph, pl;
+        for (int c = 0; c < VC; ++c) acc[c] *= corr;
+      }
+      m = mx;
+      // weights times 2^15 (in the range of fp16) as a rounded value and a rest: 22 bits
+      u32x4 ph, pl;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float e0 = __builtin_amdgcn_exp2f(sc[2 * i] - safe) * 32768.f, e1 = __builtin_amdgcn_exp2f(sc[2 * i + 1] - safe) * 32768.f;
-          l += e0 + e1;
-          const spl_h2 hi = {(half_t)e0, (half_t)e1};
-          const spl_h2 lo = {(half_t)(e0 - (float)hi[0]), (half_t)(e1 - (float)hi[1])};
-          ph[i] = __builtin_bit_cast(unsigned, hi);
-          pl[i] = __builtin_bit_cast(unsigned, lo);
-        }
-        vwords vw[8];
+      for (int i = 0; i < 4; ++i) {
+        const float e0 = __builtin_amdgcn_exp2f(sc[2 * i] - safe) * 32768.f, e1 = __builtin_amdgcn_exp2f(sc[2 * i + 1] - safe) * 32768.f;
+        l += e0 + e1;
+        const spl_h2 hi = {(half_t)e0, (half_t)e1};
+        const spl_h2 lo = {(half_t)(e0 - (float)hi[0]), (half_t)(e1 - (float)hi[1])};
+        ph[i] = __builtin_bit_cast(unsigned, hi);
+        pl[i] = __builtin_bit_cast(unsigned, lo);
+      }
+      vwords vw[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) vw[j] = __builtin_bit_cast(vwords, vr[j]);
+      for (int j = 0; j < 8; ++j) vw[j] = __builtin_bit_cast(vwords, vr[j]);
 #pragma unroll
-        for (int c = 0; c < VC; ++c) {
-          u32x4 a;
+      for (int c = 0; c < VC; ++c) {
+        u32x4 a;
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            a[i] = __builtin_amdgcn_perm(vw[2 * i + 1][c / 2], vw[2 * i][c / 2], c % 2 ? 0x07060302u : 0x05040100u);
-          const half8 a8 = __builtin_bit_cast(half8, a);
-          acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a8, __builtin_bit_cast(half8, pl), acc[c], 0, 0, 0);
-          acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a8, __builtin_bit_cast(half8, ph), acc[c], 0, 0, 0);
-        }
+        for (int i = 0; i < 4; ++i)
+          a[i] = __builtin_amdgcn_perm(vw[2 * i + 1][c / 2], vw[2 * i][c / 2], c % 2 ? 0x07060302u : 0x05040100u);
+        const half8 a8 = __builtin_bit_cast(half8, a);
+        acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a8, __builtin_bit_cast(half8, pl), acc[c], 0, 0, 0);
+        acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a8, __builtin_bit_cast(half8, ph), acc[c], 0, 0, 0);
       }
       __builtin_amdgcn_sched_barrier(0);  // with the products and the next rows' addresses mixed, registers spill
-      if (t + 1 < t1) {
-        k0 = paged_tile_start<SPL_TILE>(tl, t + 1) + wave * SPL_STEP;
-        if (k0 <= last) fetch(k0);
-        ids(t + 2);
+      if (t + SPL_WAVES < end) {
+        k0 = paged_tile_start<SPL_STEP>(tl, t + SPL_WAVES);
+        fetch(k0);
+        ids(t + 2 * SPL_WAVES);
       }
     }
     l += __shfl_xor(l, 16, AF_WAVE);
@@ -227,7 +225,7 @@ __device__ __forceinline__ void paged_split_body(const PagedSplitParams& p, cons
     }
     __syncthreads();
     const u64 start = u - (u64)t0;
-    const bool whole = t1 - t0 == tiles;
+    const bool whole = t1 - t0 == units;
     // A result that is not a number (an infinity among what was read, seen or not; nothing seen) is formed again key by key.
     auto store = [&](int rr, float v0, float v1, float L) __attribute__((always_inline)) {
       const int ra = r0 + rr, ta = ra / rep, ha = kvh * rep + (ra - ta * rep), d = lane * 2;
@@ -331,7 +329,7 @@ __device__ __forceinline__ void paged_split_body(const PagedSplitParams& p, cons
     if (!whole) {
       // Workgroups w0 .. w1 have the group's pieces.  Sixteen neighbours join theirs, and where there are more of them, the
       // sixteens' sums are joined after that: a single workgroup would go through 64 pieces of eight rows for 17 us.
-      const int w0 = (int)(start / share), w1 = (int)((start + (u64)tiles - 1) / share);
+      const int w0 = (int)(start / share), w1 = (int)((start + (u64)units - 1) / share);
       const int first = w0 + (wg - w0) / SPL_JOIN * SPL_JOIN, cnt = min(SPL_JOIN, w1 - first + 1);
       const int sets = (w1 - w0) / SPL_JOIN + 1;
       done = true;
