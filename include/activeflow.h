@@ -373,6 +373,19 @@ int af_paged_attention(af_ctx* ctx, const af_paged_cache* cache, const af_paged_
                        float scale, int window, int n_sink, const void* q_f16, long long q_stride,
                        void* out_f16, long long out_stride);
 
+/* af_decode_layer_batch with the tokens' keys and values in a paged cache: batch->n_rows (1 .. AF_MAX_BATCH)
+ * tokens, one each of as many sequences (q_start NULL) or several of a sequence (drafted tokens, a
+ * short prompt).  pos: device int32 [n_rows] or NULL; window, n_sink: as af_paged_attention; q_gain, k_gain: gains of
+ * the heads' norms (as af_paged_append, with cfg's rms_eps), or NULL for none.  All lengths are device memory: a captured step
+ * goes on being valid while the sequences grow.  The rotated queries are rounded to fp16 between the two operators;
+ * otherwise a token's result is what af_decode_layer_batch gives for it.  Rows without a token (padding, reported ranges) get
+ * values without meaning, the others' do not depend on them. */
+int af_decode_layer_batch_paged(af_ctx* ctx, const af_layer_cfg* cfg, const af_layer_weights* w,
+                                const void* hidden_in, void* hidden_out, const af_paged_cache* cache,
+                                const af_paged_batch* batch, const int32_t* pos, int window, int n_sink,
+                                const void* q_gain_f16, const void* k_gain_f16, const af_select_cfg* sel,
+                                af_idx_sets* sets, int32_t* union_n);
+
 /* n_layers layers in sequence.  w, k_caches, v_caches, sets: host arrays of n_layers
  * entries.  With group > 1, layer l with l % group != 0 reuses the sets of its group's
  * first layer at the points named by reuse_points (Section 3, N = 4); sets[l] of a

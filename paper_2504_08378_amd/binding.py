@@ -40,7 +40,7 @@ EXPORTS = [
     "af_cost_eval", "af_plan_search", "af_sparse_gemv_f16_noalloc",
     "af_profile_set", "af_wall_clock_khz", "af_set_option", "af_last_device_error",
     "af_unpack_q4_g32", "af_probe_stream_read_variant", "af_decode_layer_batch",
-    "af_paged_append", "af_paged_attention",
+    "af_paged_append", "af_paged_attention", "af_decode_layer_batch_paged",
 ]
 AF_MOE_MAX_EXPERTS, AF_MOE_MAX_TOP = 16, 4
 
@@ -162,6 +162,9 @@ def lib() -> C.CDLL:
         "af_decode_layer_batch": (i, [vp, C.POINTER(LayerCfg), C.POINTER(LayerWeights), i, vp, vp,
                                       C.POINTER(vp), C.POINTER(vp), C.POINTER(i), i, C.POINTER(i),
                                       C.POINTER(SelectCfg), C.POINTER(IdxSets), vp]),
+        "af_decode_layer_batch_paged": (i, [vp, C.POINTER(LayerCfg), C.POINTER(LayerWeights), vp, vp,
+                                            C.POINTER(PagedCacheStruct), C.POINTER(PagedBatchStruct), vp, i, i, vp, vp,
+                                            C.POINTER(SelectCfg), C.POINTER(IdxSets), vp]),
         "af_paged_append": (i, [vp, C.POINTER(PagedCacheStruct), C.POINTER(PagedBatchStruct), i, f, vp, vp, f, vp,
                                 vp, C.c_longlong, vp, C.c_longlong]),
         "af_paged_attention": (i, [vp, C.POINTER(PagedCacheStruct), C.POINTER(PagedBatchStruct), i, f, i, i, vp,
@@ -508,6 +511,21 @@ class Context:
             _ptr(hidden_out, torch.float16, "hidden_out"), kp, vp_, kl, kv_cap, ps, C.byref(sel),
             C.byref(sets), _ptr(union_n, torch.int32, "union_n")), "af_decode_layer_batch")
 
+    def decode_layer_batch_paged(self, cfg: LayerCfg, w: LayerWeights, hidden_in, hidden_out, cache: PagedCache,
+                                 batch: PagedBatch, sel: SelectCfg, sets: IdxSets, union_n=None, pos=None, window: int = 0,
+                                 n_sink: int = 0, q_gain=None, k_gain=None):
+        """decode_layer_batch over a paged cache: hidden_in / hidden_out fp16 [batch.n_rows][d]."""
+        self._paged_check(cache, batch)
+        for t, name in ((hidden_in, "hidden_in"), (hidden_out, "hidden_out")):
+            if t.numel() != batch.n_rows * cfg.d_model:
+                raise TypeError(f"{name} must be [{batch.n_rows}][{cfg.d_model}]")
+        self._paged_extras(batch, cache.head_dim, q_gain, k_gain, pos)
+        _check(lib().af_decode_layer_batch_paged(
+            self._h, C.byref(cfg), C.byref(w), _ptr(hidden_in, torch.float16, "hidden_in"),
+            _ptr(hidden_out, torch.float16, "hidden_out"), cache._ref, batch._ref, _ptr(pos, torch.int32, "pos"), window,
+            n_sink, _ptr(q_gain, torch.float16, "q_gain"), _ptr(k_gain, torch.float16, "k_gain"), C.byref(sel),
+            C.byref(sets), _ptr(union_n, torch.int32, "union_n")), "af_decode_layer_batch_paged")
+
     def decode_stack(self, cfg: LayerCfg, w_array, n_layers: int, hidden_in, hidden_out,
                      k_ptrs, v_ptrs, kv_len: int, kv_cap: int, pos: int, sel,
                      group: int, reuse_points: int, sets_array):
@@ -566,6 +584,11 @@ class Context:
         if cache.index != self.device.index or batch.index != self.device.index:
             raise TypeError("cache and batch must be on the context's device")
 
+    def _paged_extras(self, batch: PagedBatch, hd: int, q_gain, k_gain, pos):
+        for t, n, name in ((q_gain, hd, "q_gain"), (k_gain, hd, "k_gain"), (pos, batch.n_rows, "pos")):
+            if t is not None and (t.numel() < n or t.get_device() != self.device.index):
+                raise TypeError(f"{name} must have {n} entries on the context's device")
+
     def paged_append(self, cache: PagedCache, batch: PagedBatch, qkv, q_out, n_heads: int, rope_theta: float = 10000.0,
                      q_gain=None, k_gain=None, eps: float = 1e-5, pos=None):
         """Store the new tokens' keys and values in their pages.  qkv [n_rows][(n_heads + 2 kv heads) head_dim]; q_out
@@ -574,11 +597,7 @@ class Context:
         hd = cache.head_dim
         src, src_ld = self._paged_rows(qkv, batch.n_rows, (n_heads + 2 * cache.n_kv_heads) * hd, "qkv")
         dst, dst_ld = (None, 0) if q_out is None else self._paged_rows(q_out, batch.n_rows, n_heads * hd, "q_out")
-        for t, name in ((q_gain, "q_gain"), (k_gain, "k_gain")):
-            if t is not None and (t.numel() != hd or t.device != self.device):
-                raise TypeError(f"{name} must have {hd} entries on the context's device")
-        if pos is not None and (pos.numel() < batch.n_rows or pos.device != self.device):
-            raise TypeError(f"pos must have at least {batch.n_rows} entries on the context's device")
+        self._paged_extras(batch, hd, q_gain, k_gain, pos)
         _check(lib().af_paged_append(self._h, cache._ref, batch._ref, n_heads, rope_theta,
                                      _ptr(q_gain, torch.float16, "q_gain"), _ptr(k_gain, torch.float16, "k_gain"), eps,
                                      _ptr(pos, torch.int32, "pos"), src, src_ld, dst, dst_ld), "af_paged_append")

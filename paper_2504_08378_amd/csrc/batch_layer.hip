@@ -10,10 +10,11 @@
 // token) and stores a bit per channel; one launch turns the tokens' bits into the union and the masked
 // token values; one launch streams the union's weight rows for all tokens.  Attention is one launch
 // over (key head with up to eight of its query heads, key split, token); each token has its own
-// cache, length and position.
+// cache, length and position.  With a paged cache (af_decode_layer_batch_paged) it is two, the append and the attention.
 #include <math.h>
 
 #include "af_internal.h"
+#include "paged.h"
 #include "row_prologue.h"
 
 #define BS_THREADS 1024
@@ -75,14 +76,9 @@ static int launch_batch_select(af_ctx* ctx, int B, int producer, const half_t* s
   return AF_OK;
 }
 
-extern "C" int af_decode_layer_batch(af_ctx* ctx, const af_layer_cfg* cfg, const af_layer_weights* w,
-                                     int B, const void* hidden_in, void* hidden_out,
-                                     void* const* k_caches, void* const* v_caches, const int* kv_len,
-                                     int kv_cap, const int* pos, const af_select_cfg* sel,
-                                     af_idx_sets* sets, int32_t* union_n) {
-  if (!ctx || !cfg || !w || !hidden_in || !hidden_out || !k_caches || !v_caches || !kv_len || !pos ||
-      !sel || !sets)
-    return AF_ENULL;
+// What both entry points refuse of the layer itself.
+static int batch_layer_check(const af_layer_cfg* cfg, const af_layer_weights* w, int B, const af_select_cfg* sel,
+                             const af_idx_sets* sets) {
   if (B < 1 || B > AF_MAX_BATCH) return AF_EINVAL;
   if (cfg->d_model <= 0 || cfg->n_heads <= 0 || cfg->n_kv_heads <= 0 || cfg->d_ffn <= 0) return AF_EINVAL;
   if (cfg->head_dim != 128 && cfg->head_dim != 64) return AF_ESHAPE;
@@ -93,7 +89,7 @@ extern "C" int af_decode_layer_batch(af_ctx* ctx, const af_layer_cfg* cfg, const
   if (sel->reuse_mask) return AF_EINVAL;
   if (!w->Wqkv || !w->Wo || !w->Wgateup || !w->Wdown || !w->g_attn_norm || !w->g_ffn_norm) return AF_ENULL;
   const int d = cfg->d_model, f = cfg->d_ffn, hd = cfg->head_dim;
-  const int qdim = cfg->n_heads * hd, qkv_out = (cfg->n_heads + 2 * cfg->n_kv_heads) * hd;
+  const int qdim = cfg->n_heads * hd;
   const int widths[4] = {d, qdim, d, f};
   for (int p = 0; p < 4; ++p) {
     if (widths[p] > AF_MAX_N) return AF_ESHAPE;
@@ -101,14 +97,20 @@ extern "C" int af_decode_layer_batch(af_ctx* ctx, const af_layer_cfg* cfg, const
     if (sel->mode == AF_SEL_TOPK && (sel->k[p] < 0 || sel->k[p] > widths[p])) return AF_EINVAL;
     if (sel->mode == AF_SEL_THRESHOLD && sel->t[p] != sel->t[p]) return AF_EINVAL;
   }
-  if (kv_cap <= 0) return AF_EINVAL;
-  for (int b = 0; b < B; ++b) {
-    if (!k_caches[b] || !v_caches[b]) return AF_ENULL;
-    if (kv_len[b] < 0 || kv_len[b] >= kv_cap || pos[b] < 0) return AF_EINVAL;
-  }
-  if (!ctx->ws) return AF_EWORKSPACE;
+  return AF_OK;
+}
+
+// The layer behind its entry points' own checks.  attention(qkv, scratch, out): rotation, append and attention of the B
+// tokens, scratch being an unused [B][n_heads * head_dim].
+template <class Attention>
+static int batch_layer(af_ctx* ctx, const af_layer_cfg* cfg, const af_layer_weights* w, int B, const void* hidden_in,
+                       void* hidden_out, const af_select_cfg* sel, af_idx_sets* sets, int32_t* union_n,
+                       Attention&& attention) {
+  const int d = cfg->d_model, f = cfg->d_ffn, hd = cfg->head_dim;
+  const int qdim = cfg->n_heads * hd, qkv_out = (cfg->n_heads + 2 * cfg->n_kv_heads) * hd;
   const int max_w = qkv_out > 2 * f ? qkv_out : 2 * f;
   const int max_i = f > qdim ? f : qdim;
+  if (!ctx->ws) return AF_EWORKSPACE;
   if (max_i > ctx->max_in || d > ctx->max_in || max_w > ctx->max_out || B > ctx->max_batch)
     return AF_EWORKSPACE;
 
@@ -149,9 +151,7 @@ extern "C" int af_decode_layer_batch(af_ctx* ctx, const af_layer_cfg* cfg, const
                                 cfg->rms_eps, d, sel, 0, x0, sets->idx[0], sets->count[0])))
     return rc;
   if ((rc = gemv(0, w->Wqkv, d, qkv_out, x0, qkv, nullptr))) return rc;
-  if ((rc = af_launch_attention_batch(ctx, cfg, B, qkv, qkv_out, k_caches, v_caches, kv_len, kv_cap, pos,
-                                      attn, qdim)))
-    return rc;
+  if ((rc = attention(qkv, x3, attn))) return rc;
   // o + residual
   if ((rc = launch_batch_select(ctx, B, AF_PRO_NONE, attn, qdim, nullptr, 0.f, qdim, sel, 1, nullptr,
                                 sets->idx[1], sets->count[1])))
@@ -168,4 +168,49 @@ extern "C" int af_decode_layer_batch(af_ctx* ctx, const af_layer_cfg* cfg, const
     return rc;
   if ((rc = gemv(3, w->Wdown, f, d, x3, h_out, hmid))) return rc;
   return AF_OK;
+}
+
+extern "C" int af_decode_layer_batch(af_ctx* ctx, const af_layer_cfg* cfg, const af_layer_weights* w,
+                                     int B, const void* hidden_in, void* hidden_out,
+                                     void* const* k_caches, void* const* v_caches, const int* kv_len,
+                                     int kv_cap, const int* pos, const af_select_cfg* sel,
+                                     af_idx_sets* sets, int32_t* union_n) {
+  if (!ctx || !cfg || !w || !hidden_in || !hidden_out || !k_caches || !v_caches || !kv_len || !pos ||
+      !sel || !sets)
+    return AF_ENULL;
+  int rc = batch_layer_check(cfg, w, B, sel, sets);
+  if (rc != AF_OK) return rc;
+  if (kv_cap <= 0) return AF_EINVAL;
+  for (int b = 0; b < B; ++b) {
+    if (!k_caches[b] || !v_caches[b]) return AF_ENULL;
+    if (kv_len[b] < 0 || kv_len[b] >= kv_cap || pos[b] < 0) return AF_EINVAL;
+  }
+  const int qdim = cfg->n_heads * cfg->head_dim, qkv_out = qdim + 2 * cfg->n_kv_heads * cfg->head_dim;
+  return batch_layer(ctx, cfg, w, B, hidden_in, hidden_out, sel, sets, union_n, [&](half_t* qkv, half_t*, half_t* attn) {
+    return af_launch_attention_batch(ctx, cfg, B, qkv, qkv_out, k_caches, v_caches, kv_len, kv_cap, pos, attn, qdim);
+  });
+}
+
+extern "C" int af_decode_layer_batch_paged(af_ctx* ctx, const af_layer_cfg* cfg, const af_layer_weights* w,
+                                           const void* hidden_in, void* hidden_out, const af_paged_cache* cache,
+                                           const af_paged_batch* batch, const int32_t* pos, int window, int n_sink,
+                                           const void* q_gain_f16, const void* k_gain_f16, const af_select_cfg* sel,
+                                           af_idx_sets* sets, int32_t* union_n) {
+  if (!ctx || !cfg || !w || !hidden_in || !hidden_out || !cache || !batch || !sel || !sets) return AF_ENULL;
+  const int B = batch->n_rows;
+  int rc = batch_layer_check(cfg, w, B, sel, sets);
+  if (rc != AF_OK) return rc;
+  if (cache->n_kv_heads != cfg->n_kv_heads || cache->head_dim != cfg->head_dim) return AF_ESHAPE;
+  if (window < 0 || n_sink < 0 || !(cfg->rope_theta > 0.f) || !(cfg->rope_theta < INFINITY)) return AF_EINVAL;
+  if (!(cfg->rms_eps >= 0.f) || !(cfg->rms_eps < INFINITY)) return AF_EINVAL;
+  if (((uintptr_t)q_gain_f16 | (uintptr_t)k_gain_f16) & 15u) return AF_ESHAPE;
+  PagedView v;  // what the two operators would refuse, before anything is launched
+  if ((rc = af_paged_view(cache, batch, cfg->n_heads, &v)) != AF_OK || (rc = af_paged_ready(ctx, &v)) != AF_OK) return rc;
+  const int qdim = cfg->n_heads * cfg->head_dim, qkv_out = qdim + 2 * cfg->n_kv_heads * cfg->head_dim;
+  return batch_layer(ctx, cfg, w, B, hidden_in, hidden_out, sel, sets, union_n, [&](half_t* qkv, half_t* q, half_t* attn) {
+    const int e = af_paged_append(ctx, cache, batch, cfg->n_heads, cfg->rope_theta, q_gain_f16, k_gain_f16, cfg->rms_eps, pos,
+                                  qkv, qkv_out, q, qdim);
+    if (e != AF_OK) return e;
+    return af_paged_attention(ctx, cache, batch, cfg->n_heads, 0.f, window, n_sink, q, qdim, attn, qdim);
+  });
 }

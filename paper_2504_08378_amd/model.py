@@ -226,3 +226,50 @@ class DeviceMoeLayer:
     def run(self, hidden_in, hidden_out, K, V, kv_len: int, kv_cap: int, pos: int, sel: B.SelectCfg):
         self.ctx.decode_moe_layer(self.cfg, self.weights_struct(), hidden_in, hidden_out, K, V, kv_len,
                                   kv_cap, pos, sel, self.sets_struct(), self.route_struct())
+
+
+class PagedKv:
+    """Paged keys and values of n_layers layers that share one page table: the pages, the table and lengths on the device,
+    and the host's book of which pages are free.  Sequences are numbers 0 .. max_seqs - 1."""
+
+    def __init__(self, ctx: B.Context, shape, n_layers: int, n_pages: int, page_tokens: int = 64, max_seqs: int = B.AF_MAX_BATCH,
+                 max_tokens: int = 4096):
+        self.ctx, self.page_tokens = ctx, page_tokens
+        dims = (n_pages, shape.n_kv_heads, page_tokens, shape.head_dim)
+        new = lambda: torch.zeros(dims, dtype=torch.float16, device=ctx.device)
+        self.layers = [B.PagedCache(new(), new()) for _ in range(n_layers)]
+        self.table = torch.full((max_seqs, -(-max_tokens // page_tokens)), -1, dtype=torch.int32, device=ctx.device)
+        self.kv_len = torch.zeros(max_seqs, dtype=torch.int32, device=ctx.device)
+        self.pages = [[] for _ in range(max_seqs)]
+        self.lens = [0] * max_seqs
+        self.free_pages = list(range(n_pages - 1, -1, -1))
+        torch.cuda.current_stream(ctx.device).synchronize()
+
+    def extend(self, counts):
+        """Room for counts[b] new tokens of sequence b (0: none); queues the new table entries and lengths on the context's
+        stream and returns the batch of those tokens: one of one token each if every sequence has one."""
+        need = [-(-(n + c) // self.page_tokens) - len(p) for n, c, p in zip(self.lens, counts, self.pages)]
+        if len(counts) != len(self.lens) or min(counts) < 0:
+            raise ValueError(f"counts must hold {len(self.lens)} numbers that are not negative")
+        if sum(n for n in need if n > 0) > len(self.free_pages):
+            raise MemoryError("no pages left")
+        if max(len(p) + n for p, n in zip(self.pages, need)) > self.table.shape[1]:
+            raise ValueError("a sequence is longer than its row of the page table")
+        for b, c in enumerate(counts):
+            self.pages[b] += [self.free_pages.pop() for _ in range(need[b])]
+            self.lens[b] += c
+        with torch.cuda.stream(self.ctx.stream):
+            host = torch.full(tuple(self.table.shape), -1, dtype=torch.int32)
+            for b, p in enumerate(self.pages):
+                host[b, : len(p)] = torch.tensor(p, dtype=torch.int32)
+            self.table.copy_(host)
+            self.kv_len.copy_(torch.tensor(self.lens, dtype=torch.int32))
+            if all(c == 1 for c in counts):
+                return B.PagedBatch(self.table, self.kv_len)
+            start = torch.tensor([0] + list(np.cumsum(counts)), dtype=torch.int32).to(self.ctx.device)
+        return B.PagedBatch(self.table, self.kv_len, start, sum(counts), max(max(counts), 1))
+
+    def release(self, b: int):
+        """Sequence b has ended: its pages are free again."""
+        self.free_pages += self.pages[b][::-1]
+        self.pages[b], self.lens[b] = [], 0
