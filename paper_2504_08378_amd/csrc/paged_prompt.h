@@ -1,7 +1,8 @@
 // Attention of prompts over a paged cache: many rows of a sequence at a time, on the matrix cores.
 //
 // A workgroup has 128 rows, (token, query head) pairs that share a key head, and goes through the keys that any of
-// them sees, 64 at a time; a wave has 32 of the rows.
+// them sees, 64 at a time (four sixteens, each in one page: the first tokens and a window make one list); a wave has 32 of
+// the rows.
 //   scores   S^T[key][row] = K Q^T, 32 x 32 per instruction: a row's scores lie in the registers of two lanes;
 //   values   O^T[dim][row] = V^T P^T: which eight keys a lane supplies per instruction is free as long as both operands
 //            agree, so it supplies those whose weights it has; V comes out of LDS transposed.
@@ -24,7 +25,8 @@
 
 #define PRM_WAVES 4
 #define PRM_ROWS (32 * PRM_WAVES)
-#define PRM_TILE 64
+#define PRM_SPAN 16                        // keys that a wave loads of a tile: never in two pages
+#define PRM_TILE (PRM_WAVES * PRM_SPAN)
 typedef float prm_f16 __attribute__((ext_vector_type(16)));
 typedef half_t prm_h2 __attribute__((ext_vector_type(2)));
 typedef half_t prm_h4 __attribute__((ext_vector_type(4)));
@@ -40,8 +42,7 @@ __device__ __forceinline__ void paged_prompt_body(const PagedAttnParams& p, cons
   constexpr int DB = HD / 32;        // blocks of 32 dimensions
   constexpr int CH = HD / 8;         // 16-byte pieces of a row
   constexpr int RPI = AF_WAVE / CH;  // rows of a load instruction
-  constexpr int KEYS = PRM_TILE / PRM_WAVES;  // keys of a tile that a wave loads
-  constexpr int NI = KEYS / RPI;          // in so many instructions
+  constexpr int NI = PRM_SPAN / RPI; // load instructions of a wave per tile
   __shared__ int s_gone;  // a page of this workgroup does not exist
 
   const PagedView& v = p.v;
@@ -74,7 +75,8 @@ __device__ __forceinline__ void paged_prompt_body(const PagedAttnParams& p, cons
   const int wr0 = min(r0 + wave * 32, r1), wr1 = min(r0 + wave * 32 + 31, r1);
   const int r = min(r0 + wave * 32 + n, r1), tok = r / rep, head = kvh * rep + (r - tok * rep), place = p0 + tok;
   const int wp0 = p0 + wr0 / rep, wp1 = p0 + wr1 / rep;  // places of the wave's rows
-  const PagedTiles tl = paged_tiles<PRM_TILE>(p0 + r0 / rep, p0 + r1 / rep, window, n_sink);
+  const PagedTiles tl = paged_tiles<PRM_SPAN>(p0 + r0 / rep, p0 + r1 / rep, window, n_sink);
+  const int tiles = (tl.n + PRM_WAVES - 1) / PRM_WAVES;
 
   half8 q[KS];
   const half_t* qsrc = p.q + (size_t)(seq.row0 + tok) * p.q_stride + (size_t)head * HD + h * 8;
@@ -93,7 +95,7 @@ __device__ __forceinline__ void paged_prompt_body(const PagedAttnParams& p, cons
   size_t page_k, page_v;
   int id_next;
   auto page_of = [&](int t) __attribute__((always_inline)) {
-    return table[min(paged_tile_start<PRM_TILE>(tl, min(t, tl.n - 1)) + wave * KEYS, last) >> v.page_shift];
+    return table[paged_tile_start<PRM_SPAN>(tl, min(t * PRM_WAVES + wave, tl.n - 1)) >> v.page_shift];
   };
   auto turn_page = [&]() __attribute__((always_inline)) {
     int id = __builtin_amdgcn_readfirstlane(id_next);
@@ -105,12 +107,12 @@ __device__ __forceinline__ void paged_prompt_body(const PagedAttnParams& p, cons
     page_v = page_k;
     page_k = (size_t)id * (size_t)v.page_stride + ((size_t)kvh << v.page_shift) * HD;
   };
-  // Load instruction i of tile t's, and behind the last tile of that tile's once more.
+  // Load instruction i of tile t's, and behind the last keys of those once more.
   auto fetch = [&](const half_t* page, int t, half_t* to, int i, bool keys) __attribute__((always_inline)) {
-    const int row = wave * KEYS + i * RPI + lr;
-    const unsigned o = (unsigned)(min(paged_tile_start<PRM_TILE>(tl, min(t, tl.n - 1)) + row, last) & mask) * HD;
+    const int row = i * RPI + lr, k0 = paged_tile_start<PRM_SPAN>(tl, min(t * PRM_WAVES + wave, tl.n - 1));
+    const unsigned o = (unsigned)(min(k0 + row, last) & mask) * HD;
     const int c = lc ^ (keys ? row & (CH - 1) : HD == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2);
-    __builtin_amdgcn_global_load_lds((prm_glb*)(page + (o + c * 8)), (prm_lds*)(to + (wave * KEYS + i * RPI) * HD), 16, 0, 0);
+    __builtin_amdgcn_global_load_lds((prm_glb*)(page + (o + c * 8)), (prm_lds*)(to + (wave * PRM_SPAN + i * RPI) * HD), 16, 0, 0);
   };
   // Reads: a key's row for the scores; four keys of one dimension for the values.  The lane's places are kept as numbers that
   // the compiler does not look into: it takes reads whose address it cannot trace to one buffer for reads of what is being
@@ -143,21 +145,24 @@ __device__ __forceinline__ void paged_prompt_body(const PagedAttnParams& p, cons
 
   // Scores that a row does not see, behind the products of tile t.
   auto hide = [&](int t, prm_f16 (&s)[2]) __attribute__((always_inline)) {
-    const int k0 = paged_tile_start<PRM_TILE>(tl, t);
-    if (!(k0 + PRM_TILE - 1 <= wp0 && (window <= 0 || k0 > wp1 - window || k0 + PRM_TILE <= n_sink))) {
-      const int end = place - k0 - 4 * h, from = (window > 0 ? place - window + 1 : 0) - k0 - 4 * h, first = n_sink - k0 - 4 * h;
+    const int first = t * PRM_WAVES, k0 = paged_tile_start<PRM_SPAN>(tl, first);
+    const bool whole = first >= tl.sinks || first + PRM_WAVES <= tl.sinks;  // 64 neighbours
+    if (!(whole && k0 + PRM_TILE - 1 <= wp0 && (window <= 0 || k0 > wp1 - window || k0 + PRM_TILE <= n_sink))) {
+      const int from = window > 0 ? max(0, place - window + 1) : 0;
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
+      for (int g = 0; g < PRM_WAVES; ++g) {
+        const int k = paged_tile_start<PRM_SPAN>(tl, first + g) + 4 * h, top = place - k, low = from - k, sink = n_sink - k;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int row = kb * 32 + (i & 3) + 8 * (i >> 2);
-          s[kb][i] = (row <= end) & ((row >= from) | (row < first)) ? s[kb][i] : -INFINITY;
+        for (int i = 0; i < 8; ++i) {
+          const int row = (i & 3) + 8 * (i >> 2), e = (g & 1) * 8 + i;
+          s[g >> 1][e] = (row <= top) & ((row >= low) | (row < sink)) ? s[g >> 1][e] : -INFINITY;
         }
+      }
     }
     if (s_gone) {
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int k = k0 + g * 16;
+      for (int g = 0; g < PRM_WAVES; ++g) {
+        const int k = paged_tile_start<PRM_SPAN>(tl, first + g);
         if (k <= last && paged_page_ok(v, __builtin_amdgcn_readfirstlane(table[k >> v.page_shift]))) continue;
 #pragma unroll
         for (int i = 0; i < 8; ++i) s[g >> 1][(g & 1) * 8 + i] = -INFINITY;
@@ -276,7 +281,7 @@ __device__ __forceinline__ void paged_prompt_body(const PagedAttnParams& p, cons
       __builtin_amdgcn_sched_barrier(0);
     });
     __builtin_amdgcn_s_setprio(0);
-    if (t < tl.n) weights(t);
+    weights(t);
     wait_loads();
     sync();
   };
@@ -291,12 +296,20 @@ __device__ __forceinline__ void paged_prompt_body(const PagedAttnParams& p, cons
   wait_loads();
   sync();
   step(std::true_type{}, 0, s_k0, s_k1, s_v1, s_v0);
-  for (int t = 1;; t += 2) {
+  for (int t = 1; t < tiles; t += 2) {
     step(std::false_type{}, t, s_k1, s_k0, s_v0, s_v1);
-    if (t >= tl.n) break;
-    step(std::false_type{}, t + 1, s_k0, s_k1, s_v1, s_v0);
-    if (t + 1 >= tl.n) break;
+    if (t + 1 < tiles) step(std::false_type{}, t + 1, s_k0, s_k1, s_v1, s_v0);
   }
+  auto finish = [&](const half_t* sv) __attribute__((always_inline)) {  // the last values
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int s4 = 0; s4 < 4; ++s4) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(value(sv, d, s4), w[s4], o[d], 0, 0, 0);
+  };
+  if (tiles & 1)
+    finish(s_v0);
+  else
+    finish(s_v1);
 
   if (r0 + wave * 32 > r1) return;
   l += __shfl_xor(l, 32, AF_WAVE);
