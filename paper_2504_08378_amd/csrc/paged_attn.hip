@@ -20,7 +20,7 @@ __global__ __launch_bounds__(SPL_THREADS, 2) void paged_split_kernel(PagedSplitP
 }
 
 template <int HD>
-__global__ __launch_bounds__(SPL_THREADS, 2) void paged_mixed_kernel(PagedSplitParams p, int wgs) {
+__global__ __launch_bounds__(SPL_THREADS, 2) void paged_mixed_kernel(PagedSplitParams p, PagedPieces pieces, int wgs, int longs) {
   static_assert(SPL_THREADS == PRM_WAVES * AF_WAVE && SPL_ROWS * (HD + 4) * sizeof(float) <= PRM_TILE * HD * sizeof(half_t), "LDS shared");
   extern __shared__ __align__(16) unsigned long long s_first[];
   __shared__ __align__(16) half_t s_k0[PRM_TILE * HD], s_k1[PRM_TILE * HD], s_v0[PRM_TILE * HD], s_v1[PRM_TILE * HD];
@@ -28,19 +28,21 @@ __global__ __launch_bounds__(SPL_THREADS, 2) void paged_mixed_kernel(PagedSplitP
     float* const acc[SPL_WAVES] = {(float*)s_k0, (float*)s_k1, (float*)s_v0, (float*)s_v1};
     paged_split_body<HD>(p, blockIdx.x, wgs, acc, s_first);
   } else {
-    paged_prompt_body<HD>(p.a, p.short_q, blockIdx.x - (unsigned)wgs, s_k0, s_k1, s_v0, s_v1);
+    const unsigned wg = blockIdx.x - (unsigned)wgs;
+    const int piece = pieces.most > 1 ? (int)(wg / (unsigned)longs) : 0;
+    paged_prompt_body<HD>(p.a, pieces, p.short_q, wg - (unsigned)(piece * longs), piece, s_k0, s_k1, s_v0, s_v1);
   }
 }
 
 template <int HD>
 static int launch_attention(af_ctx* ctx, const PagedAttnParams& a) {
   const int rep = a.n_heads / a.v.n_kv, short_q = rep < SPL_ROWS ? SPL_ROWS / rep : 1;
-  const bool mixed = a.v.max_q_len > short_q;
+  const bool mixed = a.v.max_q_len > short_q && a.v.n_rows > short_q;
   PagedSplitParams p;
   p.a = a;
   p.part = (float*)(ctx->ws + ctx->lay.partials);
   p.tickets = (int*)(ctx->ws + ctx->lay.tickets) + AF_TICKET_ATTN;
-  p.slot_rows = rep >= SPL_ROWS ? SPL_ROWS : rep * (mixed ? short_q : a.v.max_q_len);
+  p.slot_rows = rep >= SPL_ROWS ? SPL_ROWS : rep * (a.v.max_q_len < short_q ? a.v.max_q_len : short_q);
   p.short_q = short_q;
   const size_t floats = (ctx->lay.attn_part + ctx->lay.attn_floats * sizeof(float) - ctx->lay.partials) / sizeof(float);
   const size_t fit = floats / ((size_t)2 * p.slot_rows * (HD + 2));
@@ -56,9 +58,27 @@ static int launch_attention(af_ctx* ctx, const PagedAttnParams& a) {
   }
   // as many workgroups for the long ones as any division of the rows among the sequences can need
   const long long longer = a.v.n_rows / (short_q + 1);
-  const long long more = ((long long)a.v.n_rows * rep / PRM_ROWS + (a.v.n_seqs < longer ? a.v.n_seqs : longer)) * a.v.n_kv;
-  if (wgs + more > 0x7FFFFFFF) return AF_EINVAL;
-  hipLaunchKernelGGL(paged_mixed_kernel<HD>, dim3((unsigned)(wgs + more)), dim3(SPL_THREADS), lds, ctx->stream, p, (int)wgs);
+  const long long longs = ((long long)a.v.n_rows * rep / PRM_ROWS + (a.v.n_seqs < longer ? a.v.n_seqs : longer)) * a.v.n_kv;
+  // In pieces where they would not fill the chip, two a unit, and the keys may be many (us, whole / in pieces, 32 query heads on 8:
+  // 32 tokens behind 8000 147 / 40, 256 behind 30000 539 / 192, two times 64 behind 2000 44.5 / 25.9; 16 on 1, 100 behind 60000 1046 / 96;
+  // where the keys are few there is one piece: 500 tokens 16.6 / 17.0).
+  PagedPieces pieces{};
+  pieces.tickets = p.tickets;
+  pieces.ticket0 = 2 * SPL_MAX_WGS;
+  pieces.part = p.part + (size_t)2 * wgs * p.slot_rows * (HD + 2);
+  pieces.most = 1;
+  if (longs <= ctx->n_cu && longs <= AF_TICKET_ATTN - pieces.ticket0) {
+    const long long room = (long long)((floats - (size_t)2 * wgs * p.slot_rows * (HD + 2)) / PRM_PIECE_FLOATS(HD));
+    const long long tiles = ((long long)a.v.table_stride << a.v.page_shift) / PRM_TILE;
+    long long most = 2 * ctx->n_cu / longs;
+    if (most > PRM_MAX_PIECES) most = PRM_MAX_PIECES;
+    if (most > tiles / PRM_PIECE_TILES) most = tiles / PRM_PIECE_TILES;
+    if (most > room / longs) most = room / longs;
+    if (most > 1) pieces.most = (int)most;
+  }
+  const long long grid = wgs + longs * pieces.most;
+  if (grid > 0x7FFFFFFF) return AF_EINVAL;
+  hipLaunchKernelGGL(paged_mixed_kernel<HD>, dim3((unsigned)grid), dim3(SPL_THREADS), lds, ctx->stream, p, pieces, (int)wgs, (int)longs);
   AF_LAUNCH_CHECK();
   return AF_OK;
 }

@@ -34,16 +34,33 @@ typedef __fp16 prm_fp16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) void prm_lds;
 typedef __attribute__((address_space(1))) const void prm_glb;
 
-// s_k0 .. s_v1: LDS of PRM_TILE * HD elements each, objects of their own.
+// Where few workgroups would go through many keys, several share the rows of one, each with a piece of its tiles:
+// their maxima, sums and values meet in memory, and the one that finishes last joins them, in order.
+struct PagedPieces {
+  float* part;   // [workgroup][most][PRM_PIECE_FLOATS]
+  int* tickets;  // of the workgroups, zero between launches
+  int ticket0, most;
+};
+#define PRM_MAX_PIECES 16
+#define PRM_PIECE_TILES 8  // tiles of a piece, at least
+#define PRM_PIECE_FLOATS(HD) ((size_t)PRM_WAVES * AF_WAVE * ((HD) / 2 + 2))
+PAGED_HD int paged_pieces(int tiles, int most) {
+  const int n = tiles / PRM_PIECE_TILES;
+  return n < 1 ? 1 : n < most ? n : most;
+}
+
+// s_k0 .. s_v1: LDS of PRM_TILE * HD elements each, objects of their own.  piece: which of a workgroup's pieces.
 template <int HD>
-__device__ __forceinline__ void paged_prompt_body(const PagedAttnParams& p, const int short_q, const unsigned wg, half_t* s_k0,
-                                                  half_t* s_k1, half_t* s_v0, half_t* s_v1) {
+__device__ __forceinline__ void paged_prompt_body(const PagedAttnParams& p, const PagedPieces& pieces, const int short_q,
+                                                  const unsigned wg, const int piece, half_t* s_k0, half_t* s_k1, half_t* s_v0,
+                                                  half_t* s_v1) {
   constexpr int KS = HD / 16;        // contraction steps of the scores
   constexpr int DB = HD / 32;        // blocks of 32 dimensions
   constexpr int CH = HD / 8;         // 16-byte pieces of a row
   constexpr int RPI = AF_WAVE / CH;  // rows of a load instruction
   constexpr int NI = PRM_SPAN / RPI; // load instructions of a wave per tile
   __shared__ int s_gone;  // a page of this workgroup does not exist
+  __shared__ int s_ticket;
 
   const PagedView& v = p.v;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -76,7 +93,9 @@ __device__ __forceinline__ void paged_prompt_body(const PagedAttnParams& p, cons
   const int r = min(r0 + wave * 32 + n, r1), tok = r / rep, head = kvh * rep + (r - tok * rep), place = p0 + tok;
   const int wp0 = p0 + wr0 / rep, wp1 = p0 + wr1 / rep;  // places of the wave's rows
   const PagedTiles tl = paged_tiles<PRM_SPAN>(p0 + r0 / rep, p0 + r1 / rep, window, n_sink);
-  const int tiles = (tl.n + PRM_WAVES - 1) / PRM_WAVES;
+  const int tiles = (tl.n + PRM_WAVES - 1) / PRM_WAVES, shares = paged_pieces(tiles, pieces.most);
+  if (piece >= shares) return;
+  const int t0 = (int)((long long)tiles * piece / shares), t1 = (int)((long long)tiles * (piece + 1) / shares);
 
   half8 q[KS];
   const half_t* qsrc = p.q + (size_t)(seq.row0 + tok) * p.q_stride + (size_t)head * HD + h * 8;
@@ -288,17 +307,17 @@ __device__ __forceinline__ void paged_prompt_body(const PagedAttnParams& p, cons
   if (tid == 0) s_gone = 0;
   sync();
   page_k = 0;
-  id_next = page_of(0);
+  id_next = page_of(t0);
   turn_page();
 #pragma unroll
-  for (int i = 0; i < NI; ++i) fetch(v.k + page_k, 0, s_k0, i, true);
-  id_next = page_of(1);
+  for (int i = 0; i < NI; ++i) fetch(v.k + page_k, t0, s_k0, i, true);
+  id_next = page_of(t0 + 1);
   wait_loads();
   sync();
-  step(std::true_type{}, 0, s_k0, s_k1, s_v1, s_v0);
-  for (int t = 1; t < tiles; t += 2) {
+  step(std::true_type{}, t0, s_k0, s_k1, s_v1, s_v0);
+  for (int t = t0 + 1; t < t1; t += 2) {
     step(std::false_type{}, t, s_k1, s_k0, s_v0, s_v1);
-    if (t + 1 < tiles) step(std::false_type{}, t + 1, s_k0, s_k1, s_v1, s_v0);
+    if (t + 1 < t1) step(std::false_type{}, t + 1, s_k0, s_k1, s_v1, s_v0);
   }
   auto finish = [&](const half_t* sv) __attribute__((always_inline)) {  // the last values
 #pragma unroll
@@ -306,12 +325,52 @@ __device__ __forceinline__ void paged_prompt_body(const PagedAttnParams& p, cons
 #pragma unroll
       for (int s4 = 0; s4 < 4; ++s4) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(value(sv, d, s4), w[s4], o[d], 0, 0, 0);
   };
-  if (tiles & 1)
+  if ((t1 - t0) & 1)
     finish(s_v0);
   else
     finish(s_v1);
 
-  if (r0 + wave * 32 > r1) return;
+  const bool rows = r0 + wave * 32 <= r1;  // this wave has any
+  if (shares > 1) {
+    // a thread's pairs of values, 512 bytes of a wave next to each other: (m, l), then o
+    auto at = [&](int z, int k) __attribute__((always_inline)) {
+      return pieces.part + ((size_t)wg * pieces.most + z) * PRM_PIECE_FLOATS(HD) + ((size_t)k * PRM_WAVES * AF_WAVE + tid) * 2;
+    };
+    if (rows) {
+      af_store_agent2(at(piece, 0), m, l);
+#pragma unroll
+      for (int k = 0; k < HD / 4; ++k) af_store_agent2(at(piece, 1 + k), o[k >> 3][2 * k & 15], o[k >> 3][(2 * k & 15) + 1]);
+    }
+    af_stores_done();
+    __syncthreads();
+    if (tid == 0) {
+      int* ticket = &pieces.tickets[af_ticket_of(pieces.ticket0 + (int)wg)];
+      s_ticket = af_ticket_take(ticket);
+      if (s_ticket == shares - 1) af_ticket_reset(ticket);
+    }
+    __syncthreads();
+    if (s_ticket != shares - 1 || !rows) return;
+    m = -INFINITY;
+    for (int z = 0; z < shares; ++z) m = fmaxf(m, af_load_agent2(at(z, 0))[0]);
+    const float safe = m == -INFINITY ? 0.f : m;
+    l = 0.f;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) o[d] = prm_f16{};
+    for (int z = 0; z < shares; ++z) {
+      const af_float2 ml = af_load_agent2(at(z, 0));
+      af_float2 x[HD / 4];
+#pragma unroll
+      for (int k = 0; k < HD / 4; ++k) x[k] = af_load_agent2(at(z, 1 + k));
+      const float f = __builtin_amdgcn_exp2f(ml[0] - safe);
+      l += f * ml[1];
+#pragma unroll
+      for (int k = 0; k < HD / 4; ++k) {
+        o[k >> 3][2 * k & 15] += f * x[k][0];
+        o[k >> 3][(2 * k & 15) + 1] += f * x[k][1];
+      }
+    }
+  }
+  if (!rows) return;
   l += __shfl_xor(l, 32, AF_WAVE);
   const bool mine = r0 + wave * 32 + n <= r1;
   const float inv = 1.0f / l;

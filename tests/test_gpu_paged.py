@@ -184,6 +184,32 @@ def test_a_few_new_tokens(ctx, new):
         check(got, attend(bt, q, heads), heads, hd, weights16=True)
 
 
+@pytest.mark.parametrize("heads,kv,hd", [(4, 4, 64), (8, 2, 128), (32, 8, 128), (16, 1, 64)])
+@pytest.mark.parametrize("lens", [[(3000, 40)], [(5000, 17), (700, 130)], [(2600, 300), (1, 1), (900, 3), (40, 40)]])
+def test_few_rows_of_many_keys(ctx, heads, kv, hd, lens):
+    """Few workgroups, many keys: the rows' keys are shared out in pieces and joined; twice, for the counters; under a window that
+    leaves pieces in which rows see nothing; and with values that are not finite, which are seen by some rows only."""
+    for window, sinks in ((0, 0), (0, 0), (1500, 70)):
+        bt = Batch(lens, kv, hd, 16, seed=heads + window, stale=np.nan)
+        n, new = lens[0]
+        bt.V[bt.table[0, (n - 5) // 16], 0, (n - 5) % 16, 3] = np.inf
+        q, got = run(ctx, bt, heads, window=window, n_sink=sinks)
+        check(got, attend(bt, q, heads, window, sinks), heads, hd, weights16=True)
+
+
+def test_smallest_workspace(ctx):
+    """A workspace for one small token: fewer stretches and pieces, the same results."""
+    heads, kv, hd = 16, 1, 128
+    small = B.Context(0, max_in=64, max_out=64, max_batch=1)
+    try:
+        for lens, single in (([(9000, 1), (300, 1)], True), ([(4000, 40), (900, 1)], False)):
+            bt = Batch(lens, kv, hd, 16, seed=5, single=single)
+            q, got = run(small, bt, heads)
+            check(got, attend(bt, q, heads), heads, hd, weights16=not single)
+    finally:
+        small.close()
+
+
 @pytest.mark.parametrize("single", [True, False])
 def test_as_many_sequences_as_there_may_be(ctx, single):
     heads, kv, hd = 2, 1, 64
