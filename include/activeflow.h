@@ -333,7 +333,7 @@ typedef struct {
  *     order; rows behind q_start[n_seqs] are left as they are (a padded batch).  NULL: one new
  *     token each, row b is sequence b's; a sequence with kv_len 0 then has none (a padded batch).
  *   n_rows: rows of the token tensors; max_q_len: most rows of one sequence (a bound the host
- *     knows; n_rows == n_seqs and max_q_len == 1 where q_start is NULL).  n_rows * n_heads < 2^31.
+ *     knows; n_rows == n_seqs and max_q_len == 1 where q_start is NULL).  n_rows * n_heads <= 2^30.
  * A table entry outside [0, n_pages) that a token needs, a negative kv_len or one beyond the
  * table, a row range that is negative, outside [0, n_rows], longer than max_q_len or than kv_len:
  * reported (AF_DEVERR_PAGED) and not followed.  The token of such an entry is not stored and not
@@ -365,9 +365,10 @@ int af_paged_append(af_ctx* ctx, const af_paged_cache* cache, const af_paged_bat
  * tokens j <= p (window == 0), or those of them with j > p - window or j < n_sink (the last
  * `window`, and the first n_sink).
  *   out = sum of softmax(scale * q.k_j) v_j over the tokens it sees, 0 if there are none
- * (scale 0: 1 / sqrt(head_dim)).  Scores, softmax and sums are fp32.  Tokens that a row does not
- * see do not enter its result, whatever their key and value hold.  The result depends on the batch
- * (the split of the work follows the lengths) within rounding, and is the same from call to call.
+ * (scale 0: 1 / sqrt(head_dim)).  Scores, softmax and sums are fp32; where a sequence has several new tokens and more than 16
+ * rows a key head (query heads x new tokens), the weights enter the value products rounded to fp16, else as two fp16 values
+ * (22 bits).  Tokens that a row does not see do not enter its result, whatever their key and value hold.  The result depends on
+ * the batch (the work is divided by its lengths) within rounding, and is the same from call to call.
  * Alignment, device and workspace as af_paged_append; out must not overlap q. */
 int af_paged_attention(af_ctx* ctx, const af_paged_cache* cache, const af_paged_batch* batch, int n_heads,
                        float scale, int window, int n_sink, const void* q_f16, long long q_stride,

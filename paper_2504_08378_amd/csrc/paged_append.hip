@@ -169,7 +169,7 @@ int af_paged_view(const af_paged_cache* c, const af_paged_batch* b, int n_heads,
   if (b->n_seqs < 1 || b->n_seqs > AF_PAGED_MAX_SEQS || b->table_stride < 1) return AF_EINVAL;
   if (((long long)b->table_stride << shift) > AF_PAGED_MAX_TOKENS) return AF_EINVAL;
   if (b->n_rows < 0 || b->n_rows > AF_PAGED_MAX_ROWS || b->max_q_len < 1) return AF_EINVAL;
-  if ((long long)b->n_rows * n_heads > 0x7FFFFFFF) return AF_EINVAL;
+  if ((long long)b->n_rows * n_heads > 1 << 30) return AF_EINVAL;
   if (!b->q_start && (b->n_rows != b->n_seqs || b->max_q_len != 1)) return AF_EINVAL;
   v->k = (half_t*)c->k_pages;
   v->v = (half_t*)c->v_pages;

@@ -76,9 +76,8 @@ static int launch_attention(af_ctx* ctx, const PagedAttnParams& a) {
     if (most > room / longs) most = room / longs;
     if (most > 1) pieces.most = (int)most;
   }
-  const long long grid = wgs + longs * pieces.most;
-  if (grid > 0x7FFFFFFF) return AF_EINVAL;
-  hipLaunchKernelGGL(paged_mixed_kernel<HD>, dim3((unsigned)grid), dim3(SPL_THREADS), lds, ctx->stream, p, pieces, (int)wgs, (int)longs);
+  // (some 10^7 workgroups at most: n_rows * n_heads <= 2^30)
+  hipLaunchKernelGGL(paged_mixed_kernel<HD>, dim3((unsigned)(wgs + longs * pieces.most)), dim3(SPL_THREADS), lds, ctx->stream, p, pieces, (int)wgs, (int)longs);
   AF_LAUNCH_CHECK();
   return AF_OK;
 }
