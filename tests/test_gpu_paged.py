@@ -232,6 +232,37 @@ def test_strides_scale_and_spaced_pages(ctx, single):
         check(got, attend(bt, q, heads, scale=scale), heads, hd, weights16=not single)
 
 
+@pytest.mark.parametrize("new", [1, 2, 70])
+def test_offsets_beyond_32_bits(ctx, new):
+    """Pages and rows that lie 2^32 elements and more apart: the same bits as with near ones."""
+    heads, kv, hd = 4, 2, 64
+    far, near = (Batch([(90, new)] * 2, kv, hd, 16, seed=8, gap=gap, single=new == 1).upload() for gap in (2 ** 30, 0))
+    assert int(far.table.max()) * 2 ** 30 > 2 ** 32
+    width = heads * hd
+    x = torch.randn((far.rows, (heads + 2 * kv) * hd), device="cuda").half()
+    results = []
+    for bt in (far, near):
+        def rows_of(w):
+            apart = 2 ** 32 // (bt.rows - 1) // 8 * 8 + 8 if new < 70 and bt is far else w
+            return torch.empty((bt.rows - 1) * apart + w, dtype=torch.float16, device="cuda").as_strided((bt.rows, w), (apart, 1))
+        qkv, q, out = rows_of(x.shape[1]), rows_of(width), rows_of(width)
+        qkv.copy_(x)
+        q.fill_(5.0)
+        out.fill_(5.0)
+        torch.cuda.synchronize()
+        ctx.paged_append(bt.cache, bt.batch, qkv, q, heads)
+        ctx.paged_attention(bt.cache, bt.batch, q, out, heads)
+        ctx.synchronize()
+        assert ctx.last_device_error() == 0
+        results.append([to_host(t.contiguous()).view(np.uint16) for t in (q, out, bt.Kd, bt.Vd)])
+        del qkv, q, out
+    for a, b in zip(*results):
+        assert np.array_equal(a, b)
+    assert not np.any(results[0][1] == np.float16(5.0).view(np.uint16))
+    del far, near, bt
+    torch.cuda.empty_cache()
+
+
 @pytest.mark.parametrize("value", [np.nan, np.inf, -np.inf])
 @pytest.mark.parametrize("single", [True, False])
 def test_what_a_row_does_not_see_does_not_enter(ctx, value, single):
