@@ -97,15 +97,6 @@ __device__ __forceinline__ void paged_prompt_body(const PagedAttnParams& p, cons
   if (piece >= shares) return;
   const int t0 = (int)((long long)tiles * piece / shares), t1 = (int)((long long)tiles * (piece + 1) / shares);
 
-  half8 q[KS];
-  const half_t* qsrc = p.q + (size_t)(seq.row0 + tok) * p.q_stride + (size_t)head * HD + h * 8;
-#pragma unroll
-  for (int s = 0; s < KS; ++s) {
-    q[s] = *reinterpret_cast<const half8*>(qsrc + s * 16);
-    if (p.scale2 < 0.f) q[s] = -q[s];  // so that the largest product is the largest score
-  }
-  const float scale2 = fabsf(p.scale2);
-
   // loads: row 16 wave + i RPI + lane / CH of the tile, the piece that belongs where the lane writes
   const int lr = lane / CH, lc = lane % CH;
   const int32_t* table = v.table + (size_t)b * v.table_stride;
@@ -133,6 +124,40 @@ __device__ __forceinline__ void paged_prompt_body(const PagedAttnParams& p, cons
     const int c = lc ^ (keys ? row & (CH - 1) : HD == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2);
     __builtin_amdgcn_global_load_lds((prm_glb*)(page + (o + c * 8)), (prm_lds*)(to + (wave * PRM_SPAN + i * RPI) * HD), 16, 0, 0);
   };
+  auto sync = []() __attribute__((always_inline)) {  // lgkmcnt(0) and the barrier: loads stay in flight over it
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
+  };
+
+  // The first tile's keys and values and the second's keys are requested together; the first step waits for the first keys only
+  // (8932 rows that see 1028 keys each, us: with only the keys at first 181.4, so 178.3).
+  if (tid == 0) s_gone = 0;
+  id_next = page_of(t0);
+  const int id_second = page_of(t0 + 1);
+  sync();
+  page_k = 0;
+  turn_page();
+#pragma unroll
+  for (int i = 0; i < NI; ++i) fetch(v.k + page_k, t0, s_k0, i, true);
+  asm volatile("" ::: "memory");
+  half8 q[KS];
+  const half_t* qsrc = p.q + (size_t)(seq.row0 + tok) * p.q_stride + (size_t)head * HD + h * 8;
+#pragma unroll
+  for (int s = 0; s < KS; ++s) q[s] = *reinterpret_cast<const half8*>(qsrc + s * 16);
+  asm volatile("" ::: "memory");
+  id_next = id_second;
+  turn_page();
+#pragma unroll
+  for (int i = 0; i < NI; ++i) fetch(v.v + page_v, t0, s_v0, i, false);
+#pragma unroll
+  for (int i = 0; i < NI; ++i) fetch(v.k + page_k, t0 + 1, s_k1, i, true);
+  asm volatile("" ::: "memory");
+  const float scale2 = fabsf(p.scale2);
+
   // Reads: a key's row for the scores; four keys of one dimension for the values.  The lane's places are kept as numbers that
   // the compiler does not look into: it takes reads whose address it cannot trace to one buffer for reads of what is being
   // loaded, and waits for the loads.
@@ -167,14 +192,15 @@ __device__ __forceinline__ void paged_prompt_body(const PagedAttnParams& p, cons
     const int first = t * PRM_WAVES, k0 = paged_tile_start<PRM_SPAN>(tl, first);
     const bool whole = first >= tl.sinks || first + PRM_WAVES <= tl.sinks;  // 64 neighbours
     if (!(whole && k0 + PRM_TILE - 1 <= wp0 && (window <= 0 || k0 > wp1 - window || k0 + PRM_TILE <= n_sink))) {
-      const int from = window > 0 ? max(0, place - window + 1) : 0;
+      const int from = window > 0 ? max(0, place - window + 1) : 0, sinks = min(n_sink, from);
+      const unsigned span = (unsigned)(place - from);  // seen: from .. place, and what is below sinks
 #pragma unroll
       for (int g = 0; g < PRM_WAVES; ++g) {
-        const int k = paged_tile_start<PRM_SPAN>(tl, first + g) + 4 * h, top = place - k, low = from - k, sink = n_sink - k;
+        const int k = paged_tile_start<PRM_SPAN>(tl, first + g) + 4 * h, above = k - from, sink = sinks - k;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const int row = (i & 3) + 8 * (i >> 2), e = (g & 1) * 8 + i;
-          s[g >> 1][e] = (row <= top) & ((row >= low) | (row < sink)) ? s[g >> 1][e] : -INFINITY;
+          s[g >> 1][e] = ((unsigned)(above + row) <= span) | (row < sink) ? s[g >> 1][e] : -INFINITY;
         }
       }
     }
@@ -249,20 +275,24 @@ __device__ __forceinline__ void paged_prompt_body(const PagedAttnParams& p, cons
   };
   // m is the largest score of the tiles up to the one that set it.  While the weights of a tile stay in range (the largest below
   // 2^9 times that score's, or the sum would not be), it need not follow; if a row's do not, or it has seen nothing so far, it
-  // does, and what has been summed is scaled.  So most tiles need no maximum and no exchange between lanes.
-  auto weights = [&](int t) __attribute__((always_inline)) {
+  // does, and what has been summed is scaled.  So most tiles need no maximum and no exchange between lanes.  The first tile begins
+  // with its maximum.
+  auto weights = [&](auto first, int t) __attribute__((always_inline)) {
     hide(t, s);
-    float sum = weigh();
-    if (!__all(sum <= 65536.f && m > -INFINITY)) {
+    float sum = 0.f;
+    if constexpr (!first.value) sum = weigh();
+    if (first.value || !__all(sum <= 65536.f && m > -INFINITY)) {
       float mx = s[0][0];
 #pragma unroll
       for (int i = 1; i < 32; ++i) mx = fmaxf(mx, s[i >> 4][i & 15]);
       mx = fmaxf(fmaxf(mx, __shfl_xor(mx, 32, AF_WAVE)) * scale2, m);
-      const float corr = mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mx);
-      m = mx;
-      l *= corr;
+      if constexpr (!first.value) {
+        const float corr = mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mx);
+        l *= corr;
 #pragma unroll
-      for (int d = 0; d < DB; ++d) o[d] *= corr;
+        for (int d = 0; d < DB; ++d) o[d] *= corr;
+      }
+      m = mx;
       sum = weigh();
     }
     l += sum;
@@ -272,14 +302,6 @@ __device__ __forceinline__ void paged_prompt_body(const PagedAttnParams& p, cons
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_waitcnt(0x0F70);
     turn_page();
-  };
-  auto sync = []() __attribute__((always_inline)) {  // lgkmcnt(0) and the barrier: loads stay in flight over it
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_waitcnt(0xC07F);
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_sched_barrier(0);
-    asm volatile("" ::: "memory");
   };
 
   // Step t: products (values of t - 1, scores of t), then weights of t.  Keys of t and values of t - 1 are read in one step; the
@@ -291,6 +313,7 @@ __device__ __forceinline__ void paged_prompt_body(const PagedAttnParams& p, cons
       constexpr int PER = (2 * NI + DB - 1) / DB;
 #pragma unroll
       for (int i = d * PER; i < (d + 1) * PER && i < 2 * NI; ++i) {
+        if constexpr (first.value) break;  // requested already
         if (i < NI)
           fetch(v.v + page_v, t, v_now, i, false);
         else
@@ -300,20 +323,16 @@ __device__ __forceinline__ void paged_prompt_body(const PagedAttnParams& p, cons
       __builtin_amdgcn_sched_barrier(0);
     });
     __builtin_amdgcn_s_setprio(0);
-    weights(t);
+    weights(first, t);
     wait_loads();
     sync();
   };
-  if (tid == 0) s_gone = 0;
+  __builtin_amdgcn_s_waitcnt(0x0F70 | 2 * NI);  // vmcnt(2 NI): the first keys are there, and the queries
   sync();
-  page_k = 0;
-  id_next = page_of(t0);
-  turn_page();
+  if (p.scale2 < 0.f) {  // so that the largest product is the largest score
 #pragma unroll
-  for (int i = 0; i < NI; ++i) fetch(v.k + page_k, t0, s_k0, i, true);
-  id_next = page_of(t0 + 1);
-  wait_loads();
-  sync();
+    for (int s = 0; s < KS; ++s) q[s] = -q[s];
+  }
   step(std::true_type{}, t0, s_k0, s_k1, s_v1, s_v0);
   for (int t = t0 + 1; t < t1; t += 2) {
     step(std::false_type{}, t, s_k1, s_k0, s_v0, s_v1);
