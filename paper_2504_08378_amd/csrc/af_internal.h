@@ -363,6 +363,19 @@ __device__ __forceinline__ unsigned af_row_incl_scan(unsigned v) {
   v += (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, false);  // row_shr:8
   return v;
 }
+__device__ __forceinline__ unsigned long long af_wave_incl_scan(unsigned long long v) {
+#define AF_DPP_L(ctrl, rmask)                                                                                             \
+  ((unsigned long long)(unsigned)__builtin_amdgcn_update_dpp(0, (int)(v >> 32), ctrl, rmask, 0xf, false) << 32 |          \
+   (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, rmask, 0xf, false))
+  v += AF_DPP_L(0x111, 0xf);
+  v += AF_DPP_L(0x112, 0xf);
+  v += AF_DPP_L(0x114, 0xf);
+  v += AF_DPP_L(0x118, 0xf);
+  v += AF_DPP_L(0x142, 0xa);
+  v += AF_DPP_L(0x143, 0xc);
+#undef AF_DPP_L
+  return v;
+}
 __device__ __forceinline__ float af_wave_incl_scan(float v) {
 #define AF_DPP_F(ctrl, rmask) \
   __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), ctrl, rmask, 0xf, false))
@@ -381,6 +394,19 @@ __device__ __forceinline__ unsigned af_wave_sum(unsigned v) {
 }
 __device__ __forceinline__ float af_wave_sum(float v) {
   return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, af_wave_incl_scan(v)), 63));
+}
+
+__device__ __forceinline__ float af_wave_max(float v) {
+#define AF_DPP_F(ctrl, rmask) \
+  fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, v), __builtin_bit_cast(int, v), ctrl, rmask, 0xf, false)))
+  v = AF_DPP_F(0x111, 0xf);
+  v = AF_DPP_F(0x112, 0xf);
+  v = AF_DPP_F(0x114, 0xf);
+  v = AF_DPP_F(0x118, 0xf);
+  v = AF_DPP_F(0x142, 0xa);
+  v = AF_DPP_F(0x143, 0xc);
+#undef AF_DPP_F
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
 }
 
 // Sum eight per-lane values over the lane groups of a wave (lanes l, l + LX, l + 2 LX, ...).  Each
