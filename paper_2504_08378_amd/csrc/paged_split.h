@@ -6,10 +6,10 @@
 //   scores   D[key][row] = K Q^T: a lane supplies eight dimensions of one key, which is the load it has made;
 //   values   D[dim][row] = V^T P^T: a lane supplies the eight keys whose weights it has, picked out of the rows by byte permutation.
 // The page numbers of the next step travel with the rows of this one.
-// What bounds it: the read of the cache, 6.3 TB/s of the 6.7 of a plain read while all workgroups read (131070 keys of 8 key heads: 85 us, and 10
-// for the joins; 64 sequences of up to 8190: 112 and 3), latency where there is little (512 keys of 32 heads 9.0: 6.5 to the sums of a
-// workgroup, 2.5 for the join).  Two workgroups a compute unit (203 registers): three, with 168, 118 for the 95, four launched 127;
-// loads that stay in the caches 112.
+// What bounds it: the read of the cache, 6.4 TB/s of the 6.7 of a plain read while all workgroups read (131070 keys of 8 key heads: 84 us, and 9
+// for the joins; 64 sequences of up to 8190: 108 and 5), latency where there is little (512 keys of 32 heads 7.9: 5.9 to the sums of a
+// workgroup, 2.0 for the join).  Two workgroups a compute unit (211 registers): three, with 168, 118 for the 95 that it took then, four
+// launched 127; loads that stay in the caches 112; one of eight waves 91, but 512 keys of 32 heads 10.5 for 9.2.
 #pragma once
 #include "paged_attn.h"
 
@@ -39,7 +39,7 @@ static inline size_t paged_split_lds(int n_seqs) {
 
 // The work of the launch is a line of units, a step of each of the four waves for one group of rows, in the order sequence, key
 // head, group, key; every workgroup takes an equal stretch of it.  A group whose units lie in several stretches is joined by the
-// workgroup that finishes last.  (Stretches of single steps balance better under a window, 35.3 for 36.8 us, but cut more
+// workgroup that finishes last.  (Stretches of single steps balanced better under a window, 35.3 for the 36.8 us of then, but cut more
 // groups and put short ones on single waves: eight sequences of up to 517 keys 15.6 for 10.4, 256 of up to 1500 106 for 95.)
 // wg of wgs workgroups; acc: LDS for a wave's sums each, [SPL_ROWS][HD + 4]; s_first: LDS of paged_split_lds() bytes.
 template <int HD>
@@ -67,10 +67,11 @@ __device__ __forceinline__ void paged_split_body(const PagedSplitParams& p, cons
   const int per = (v.n_seqs + SPL_THREADS - 1) / SPL_THREADS;
   PagedSeq own{0, 0, 0};
   u64 mine = 0, total = 0, before = 0;
+  unsigned units_own = 0;  // of a group of the lane's sequence
   auto units_of = [&](const PagedSeq& s) __attribute__((always_inline)) -> u64 {
     if (s.q_len <= 0 || s.q_len > p.short_q) return 0;
-    const int units = paged_split_units(paged_tiles<SPL_STEP>(s.len - s.q_len, s.len - 1, window, n_sink));
-    return (u64)((s.q_len * rep + SPL_ROWS - 1) / SPL_ROWS) * (unsigned)v.n_kv * (u64)units;
+    units_own = paged_split_units(paged_tiles<SPL_STEP>(s.len - s.q_len, s.len - 1, window, n_sink));
+    return (u64)((s.q_len * rep + SPL_ROWS - 1) / SPL_ROWS) * (unsigned)v.n_kv * (u64)units_own;
   };
   auto of_lane = [](u64 x, int l) __attribute__((always_inline)) {
     return (u64)(unsigned)__builtin_amdgcn_readlane((int)(x >> 32), l) << 32 | (unsigned)__builtin_amdgcn_readlane((int)x, l);
@@ -101,6 +102,21 @@ __device__ __forceinline__ void paged_split_body(const PagedSplitParams& p, cons
     }
   }
   const u64 share = total >> 31 ? (total + (unsigned)wgs - 1) / (unsigned)wgs : ((unsigned)total + wgs - 1) / (unsigned)wgs;
+  // If every group can begin with a stretch of its own, it does: a workgroup then has one piece and at most one join (32 windows of
+  // 1028 keys 35.2 -> 32.2 us, 8 sequences of up to 4000 20.0 -> 19.2; 13 of up to 12102, one key head, 23.3 -> 24.3, and 0.3 to find that
+  // they cannot).
+  bool apart = false;
+  if (few && share > 1 && !(total >> 31) && (long long)v.n_seqs * v.n_kv <= wgs) {
+    const unsigned padded = (units_own + (unsigned)share - 1) / (unsigned)share * (unsigned)share;
+    const u64 wide = units_own ? mine / units_own * padded : 0;
+    const u64 up_to = af_wave_incl_scan(wide), all = of_lane(up_to, AF_WAVE - 1);
+    if (all <= (u64)wgs * share) {
+      apart = true;
+      mine = wide;
+      ends = up_to;
+      total = all;
+    }
+  }
   const u64 u0 = (u64)wg * share, u1 = min(u0 + share, total);
   if (u0 >= u1) return;
   int b = 0;
@@ -131,8 +147,9 @@ __device__ __forceinline__ void paged_split_body(const PagedSplitParams& p, cons
     const PagedTiles tl = paged_tiles<SPL_STEP>(p0, p1, window, n_sink);
     const int units = paged_split_units(tl);
     const u64 local = u - first_unit;
-    const unsigned hg = local >> 32 ? (unsigned)(local / (unsigned)units) : (unsigned)local / (unsigned)units;
-    const int t0 = (int)(local - (u64)hg * (unsigned)units), t1 = (int)min((u64)units, t0 + (u1 - u));
+    const unsigned span = apart ? ((unsigned)units + (unsigned)share - 1) / (unsigned)share * (unsigned)share : (unsigned)units;
+    const unsigned hg = local >> 32 ? (unsigned)(local / span) : (unsigned)local / span;
+    const int t0 = (int)(local - (u64)hg * span), t1 = (int)min((u64)units, t0 + (u1 - u));
     const int kvh = groups == 1 ? (int)hg : (int)(hg / (unsigned)groups), grp = (int)hg - kvh * groups;
     const int r0 = grp * SPL_ROWS, rows = min(SPL_ROWS, rows_all - r0);
 
@@ -390,7 +407,7 @@ __device__ __forceinline__ void paged_split_body(const PagedSplitParams& p, cons
       for (int i = 0; i < SPL_RW; ++i)
         if (wave + i * SPL_WAVES < rows) store(wave + i * SPL_WAVES, v0[i], v1[i], L[i]);
     }
-    u += (u64)(t1 - t0);
+    u = apart ? u1 : u + (u64)(t1 - t0);
     if (u < u1) __syncthreads();  // the sums in LDS are read; the next stretch writes them
   }
 }

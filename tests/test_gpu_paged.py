@@ -197,6 +197,17 @@ def test_few_rows_of_many_keys(ctx, heads, kv, hd, lens):
         check(got, attend(bt, q, heads, window, sinks), heads, hd, weights16=True)
 
 
+@pytest.mark.parametrize("lens", [[2900] * 16, [100 + 250 * i for i in range(16)], [700 - 5 * i for i in range(70)]])
+@pytest.mark.parametrize("new", [1, 2])
+def test_many_keys_of_many_sequences(ctx, lens, new):
+    """Several units of keys for every workgroup: as many for each sequence, as fits; for sequences that differ; for more than 64."""
+    heads, kv, hd = 16, 8, 64
+    for window, sinks in ((0, 0), (1500, 20)):
+        bt = Batch([(n, new) for n in lens], kv, hd, 64, seed=len(lens), single=new == 1)
+        q, got = run(ctx, bt, heads, window=window, n_sink=sinks)
+        check(got, attend(bt, q, heads, window=window, sinks=sinks), heads, hd)
+
+
 def test_smallest_workspace(ctx):
     """A workspace for one small token: fewer stretches and pieces, the same results."""
     heads, kv, hd = 16, 1, 128
