@@ -83,7 +83,10 @@ const char* af_strerror(int status);
  * run (top-k), or before their input is built (rows given): 0 = where the built-in rule expects a gain,
  * 1 = none, 2 = all of them that can (a top-k launch that cannot is refused with AF_EINVAL).
  * AF_OPT_MOE_ROUTER_KERNEL: 1 runs the router of af_decode_moe_layer as a launch of
- * its own instead of inside the gate|up launch. */
+ * its own instead of inside the gate|up launch.
+ * AF_OPT_PAGED_F16_WEIGHTS (default 0): with 1, af_paged_attention rounds the softmax weights of prompts (sequences with
+ * several new tokens and more than 16 rows a key head) to fp16 in front of the value products, which then take half the matrix
+ * work: faster, and each weight is off by up to 2^-11 of itself where it is otherwise by 2^-22. */
 enum {
   AF_OPT_LAYER_KERNEL = 1,
   AF_OPT_VALIDATE = 2,
@@ -93,7 +96,8 @@ enum {
   AF_OPT_TUNE_WORKGROUPS = 6,
   AF_OPT_MOE_ROUTER_KERNEL = 7,
   AF_OPT_TUNE_ATTN_SPLITS = 8,
-  AF_OPT_TUNE_EARLY_ROWS = 9
+  AF_OPT_TUNE_EARLY_ROWS = 9,
+  AF_OPT_PAGED_F16_WEIGHTS = 10
 };
 int af_set_option(af_ctx* ctx, int option, int value);
 
@@ -365,9 +369,8 @@ int af_paged_append(af_ctx* ctx, const af_paged_cache* cache, const af_paged_bat
  * tokens j <= p (window == 0), or those of them with j > p - window or j < n_sink (the last
  * `window`, and the first n_sink).
  *   out = sum of softmax(scale * q.k_j) v_j over the tokens it sees, 0 if there are none
- * (scale 0: 1 / sqrt(head_dim)).  Scores, softmax and sums are fp32; where a sequence has several new tokens and more than 16
- * rows a key head (query heads x new tokens), the weights enter the value products rounded to fp16, else as two fp16 values
- * (22 bits).  Tokens that a row does not see do not enter its result, whatever their key and value hold.  The result depends on
+ * (scale 0: 1 / sqrt(head_dim)).  Scores, softmax and sums are fp32; the weights enter the value products as two fp16 values
+ * (22 bits), unless AF_OPT_PAGED_F16_WEIGHTS is set.  Tokens that a row does not see do not enter its result, whatever their key and value hold.  The result depends on
  * the batch (the work is divided by its lengths) within rounding, and is the same from call to call.
  * Alignment, device and workspace as af_paged_append; out must not overlap q. */
 int af_paged_attention(af_ctx* ctx, const af_paged_cache* cache, const af_paged_batch* batch, int n_heads,

@@ -67,6 +67,7 @@ struct af_ctx {
   int validate;           // af_set_option(AF_OPT_VALIDATE, 1): check caller index lists on the device
   // launch-shape overrides for tuning sweeps (af_set_option; 0 = the built-in heuristic)
   int tune_lx, tune_nw, tune_split, tune_wgs, moe_router_kernel, tune_attn_splits, tune_early_rows;
+  int paged_f16_weights;  // af_set_option(AF_OPT_PAGED_F16_WEIGHTS, 1): prompts' softmax weights rounded to fp16
   int layer_kernel_state; // 0 not probed yet, 1 usable, -1 not usable on this device
   // af_paged_append: angles per position, in turns, of the last rope_theta and head width (0: none yet)
   float rope_theta;

@@ -92,6 +92,9 @@ extern "C" int af_set_option(af_ctx* ctx, int option, int value) {
     case AF_OPT_TUNE_EARLY_ROWS:
       ctx->tune_early_rows = value;
       return AF_OK;
+    case AF_OPT_PAGED_F16_WEIGHTS:
+      ctx->paged_f16_weights = value ? 1 : 0;
+      return AF_OK;
     default:
       return AF_EINVAL;
   }

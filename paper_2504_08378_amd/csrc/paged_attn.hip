@@ -19,7 +19,7 @@ __global__ __launch_bounds__(SPL_THREADS, 2) void paged_split_kernel(PagedSplitP
   paged_split_body<HD>(p, blockIdx.x, gridDim.x, acc, s_first);
 }
 
-template <int HD>
+template <int HD, bool FINE>
 __global__ __launch_bounds__(SPL_THREADS, 2) void paged_mixed_kernel(PagedSplitParams p, PagedPieces pieces, int wgs, int longs) {
   static_assert(SPL_THREADS == PRM_WAVES * AF_WAVE && SPL_ROWS * (HD + 4) * sizeof(float) <= PRM_TILE * HD * sizeof(half_t), "LDS shared");
   extern __shared__ __align__(16) unsigned long long s_first[];
@@ -30,7 +30,7 @@ __global__ __launch_bounds__(SPL_THREADS, 2) void paged_mixed_kernel(PagedSplitP
   } else {
     const unsigned wg = blockIdx.x - (unsigned)wgs;
     const int piece = pieces.most > 1 ? (int)(wg / (unsigned)longs) : 0;
-    paged_prompt_body<HD>(p.a, pieces, p.short_q, wg - (unsigned)(piece * longs), piece, s_k0, s_k1, s_v0, s_v1);
+    paged_prompt_body<HD, FINE>(p.a, pieces, p.short_q, wg - (unsigned)(piece * longs), piece, s_k0, s_k1, s_v0, s_v1);
   }
 }
 
@@ -77,7 +77,11 @@ static int launch_attention(af_ctx* ctx, const PagedAttnParams& a) {
     if (most > 1) pieces.most = (int)most;
   }
   // (some 10^7 workgroups at most: n_rows * n_heads <= 2^30)
-  hipLaunchKernelGGL(paged_mixed_kernel<HD>, dim3((unsigned)(wgs + longs * pieces.most)), dim3(SPL_THREADS), lds, ctx->stream, p, pieces, (int)wgs, (int)longs);
+  const dim3 grid((unsigned)(wgs + longs * pieces.most)), threads(SPL_THREADS);
+  if (ctx->paged_f16_weights)
+    hipLaunchKernelGGL((paged_mixed_kernel<HD, false>), grid, threads, lds, ctx->stream, p, pieces, (int)wgs, (int)longs);
+  else
+    hipLaunchKernelGGL((paged_mixed_kernel<HD, true>), grid, threads, lds, ctx->stream, p, pieces, (int)wgs, (int)longs);
   AF_LAUNCH_CHECK();
   return AF_OK;
 }

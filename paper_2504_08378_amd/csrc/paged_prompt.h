@@ -11,13 +11,17 @@
 // column of up to 16 rows, lie in different banks (the conflict counter reads 0); the loads pick the pieces from memory in
 // that order.
 //
-// What bounds it, 8192 tokens of 32 heads on 32, causal, 550 GFLOP: 573 us, 960 TFLOP/s; the matrix unit is busy 53 % of the
-// cycles, at 1.65 GHz (a loop of nothing but these instructions on random data runs at 1.6 GHz, 1650 TFLOP/s, and at 2.1 GHz on
-// zeros: power sets the clock).  On the way, us: all loads of a tile issued in a row at its start, where a wave waits until the
-// memory path has taken them, and each read next to its product 669; a maximum per tile and an exchange between the lanes 655;
-// loads between the products, with reads that the compiler could not tell from the loads' buffers (it waited for them) 667;
-// this form 573.  Eight waves on one pair of tiles, half of them a phase behind the others, 573; without the waves' priorities
-// 587.
+// The weights enter the value products as two fp16 values, 22 bits, so these are formed twice: 1.5 times the matrix work of weights
+// rounded to fp16, which leave the results 2.6e-4 from 64 bits where their own rounding leaves 2.0e-4.  The caller may choose those
+// (FINE false).
+//
+// What bounds it, 8192 tokens of 32 heads on 32, causal, 550 GFLOP: 765 us, 1080 TFLOP/s with the second value products; rounded weights
+// 580 us.  The matrix unit at the clock that power allows (a loop of nothing but these instructions on random data runs at 1.6 GHz,
+// 1650 TFLOP/s, and at 2.1 GHz on zeros), and the time when neither of the two waves of a SIMD has products ready.  On the way, us, with rounded
+// weights: all loads of a tile issued in a row at its start, where a wave waits until the memory path has taken them, and each read next
+// to its product 669; a maximum per tile and an exchange between the lanes 655; loads between the products, with reads that the compiler
+// could not tell from the loads' buffers (it waited for them) 667; this form 573.  Eight waves on one pair of tiles, half of them a phase
+// behind the others, 573; without the waves' priorities 587.
 #pragma once
 #include <type_traits>
 
@@ -28,6 +32,7 @@
 #define PRM_SPAN 16                        // keys that a wave loads of a tile: never in two pages
 #define PRM_TILE (PRM_WAVES * PRM_SPAN)
 typedef float prm_f16 __attribute__((ext_vector_type(16)));
+typedef float prm_f2 __attribute__((ext_vector_type(2)));
 typedef half_t prm_h2 __attribute__((ext_vector_type(2)));
 typedef half_t prm_h4 __attribute__((ext_vector_type(4)));
 typedef __fp16 prm_fp16x4 __attribute__((ext_vector_type(4)));
@@ -50,7 +55,8 @@ PAGED_HD int paged_pieces(int tiles, int most) {
 }
 
 // s_k0 .. s_v1: LDS of PRM_TILE * HD elements each, objects of their own.  piece: which of a workgroup's pieces.
-template <int HD>
+// FINE: weights of 22 bits, else of 11.
+template <int HD, bool FINE>
 __device__ __forceinline__ void paged_prompt_body(const PagedAttnParams& p, const PagedPieces& pieces, const int short_q,
                                                   const unsigned wg, const int piece, half_t* s_k0, half_t* s_k1, half_t* s_v0,
                                                   half_t* s_v1) {
@@ -200,7 +206,7 @@ __device__ __forceinline__ void paged_prompt_body(const PagedAttnParams& p, cons
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const int row = (i & 3) + 8 * (i >> 2), e = (g & 1) * 8 + i;
-          s[g >> 1][e] = ((unsigned)(above + row) <= span) | (row < sink) ? s[g >> 1][e] : -INFINITY;
+          s[g >> 1][e] = (((unsigned)(above + row) <= span) | (row < sink)) ? s[g >> 1][e] : -INFINITY;
         }
       }
     }
@@ -214,26 +220,30 @@ __device__ __forceinline__ void paged_prompt_body(const PagedAttnParams& p, cons
       }
     }
   };
-  half8 w[4];
+  half8 w[4], wr[FINE ? 4 : 1];  // the weights' rounded values, and what the rounding left
   // The matrix unit's half of a step: the values of tile t - 1 (sv) by its weights, the scores of tile t (keys sk).
   prm_f16 s[2];
   auto products = [&](auto first, const half_t* sk, const half_t* sv, auto&& between) __attribute__((always_inline)) {
-    half8 x[2][4], a[2][KS];
-    // Every read stands one block in front of its product; the compiler would move it next to that.
+    constexpr int AHEAD = FINE ? 3 : 4, RING = FINE ? 4 : 8;
+    half8 x[RING], a[2][KS];
+    // Every read of values stands AHEAD of its products (three pairs or four), every read of keys a block; the compiler would move
+    // it next to them.
     if constexpr (!first.value) {
 #pragma unroll
-      for (int s4 = 0; s4 < 4; ++s4) x[0][s4] = value(sv, 0, s4);
+      for (int i = 0; i < AHEAD; ++i) x[i] = value(sv, 0, i);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int d = 0; d < DB; ++d) {
 #pragma unroll
         for (int s4 = 0; s4 < 4; ++s4) {
-          if (d + 1 < DB) x[(d + 1) & 1][s4] = value(sv, d + 1, s4);
+          const int now = d * 4 + s4, next = now + AHEAD;
+          if (next < DB * 4) x[next % RING] = value(sv, next >> 2, next & 3);
           if (d + 1 == DB && s4 * 2 < KS) {
             a[0][s4 * 2] = key(sk, 0, s4 * 2);
             a[0][s4 * 2 + 1] = key(sk, 0, s4 * 2 + 1);
           }
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[d & 1][s4], w[s4], o[d], 0, 0, 0);
+          if constexpr (FINE) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[now % RING], wr[s4], o[d], 0, 0, 0);
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[now % RING], w[s4], o[d], 0, 0, 0);
           __builtin_amdgcn_sched_barrier(0);
         }
         between(d);
@@ -257,19 +267,27 @@ __device__ __forceinline__ void paged_prompt_body(const PagedAttnParams& p, cons
     for (int ks = 0; ks < KS; ++ks) s[1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[1][ks], q[ks], s[1], 0, 0, 0);
     __builtin_amdgcn_sched_barrier(0);
   };
-  // The vector unit's half: the scores to weights.  Weights times 2^7, each to the nearest of its 11 bits: one more rounding of
-  // the size of the result's own, and independent from key to key.  Returns the sum of the rounded ones.
+  // The vector unit's half: the scores to weights, times 2^7, each to the nearest of its 11 bits and, FINE, what is left to the
+  // nearest of another 11 (below 2^-32 of the row's largest weight there are none).  Without the rest each is off by 2^-11 of itself
+  // at most, independent from key to key: the caller's choice.  Returns their sum, without the rest that of the rounded ones.
   auto weigh = [&]() __attribute__((always_inline)) {
     const float off = (m == -INFINITY ? 0.f : -m) + 7.f;
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 32; i += 2) {
       const float x = s[i >> 4][i & 15], y = s[i >> 4][(i & 15) + 1];
-      const prm_h2 e = {(half_t)__builtin_amdgcn_exp2f(__builtin_fmaf(x, scale2, off)),
-                        (half_t)__builtin_amdgcn_exp2f(__builtin_fmaf(y, scale2, off))};
-      sum = __builtin_amdgcn_fdot2(e, prm_h2{(half_t)1, (half_t)1}, sum, false);
-      w[i >> 3][i & 7] = e[0];
-      w[i >> 3][(i & 7) + 1] = e[1];
+      const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x, scale2, off)), e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(y, scale2, off));
+      const prm_h2 hi = __builtin_convertvector((prm_f2{e0, e1}), prm_h2);
+      w[i >> 3][i & 7] = hi[0];
+      w[i >> 3][(i & 7) + 1] = hi[1];
+      if constexpr (FINE) {
+        const prm_h2 rest = __builtin_convertvector((prm_f2{e0 - (float)hi[0], e1 - (float)hi[1]}), prm_h2);
+        sum += e0 + e1;
+        wr[i >> 3][i & 7] = rest[0];
+        wr[i >> 3][(i & 7) + 1] = rest[1];
+      } else {
+        sum = __builtin_amdgcn_fdot2(hi, prm_h2{(half_t)1, (half_t)1}, sum, false);
+      }
     }
     return sum;
   };
@@ -281,7 +299,7 @@ __device__ __forceinline__ void paged_prompt_body(const PagedAttnParams& p, cons
     hide(t, s);
     float sum = 0.f;
     if constexpr (!first.value) sum = weigh();
-    if (first.value || !__all(sum <= 65536.f && m > -INFINITY)) {
+    if (first.value || !__all(sum <= 65504.f && m > -INFINITY)) {
       float mx = s[0][0];
 #pragma unroll
       for (int i = 1; i < 32; ++i) mx = fmaxf(mx, s[i >> 4][i & 15]);
@@ -342,7 +360,11 @@ __device__ __forceinline__ void paged_prompt_body(const PagedAttnParams& p, cons
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
-      for (int s4 = 0; s4 < 4; ++s4) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(value(sv, d, s4), w[s4], o[d], 0, 0, 0);
+      for (int s4 = 0; s4 < 4; ++s4) {
+        const half8 x = value(sv, d, s4);
+        if constexpr (FINE) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, wr[s4], o[d], 0, 0, 0);
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, w[s4], o[d], 0, 0, 0);
+      }
   };
   if ((t1 - t0) & 1)
     finish(s_v0);
