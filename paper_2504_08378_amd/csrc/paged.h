@@ -62,6 +62,10 @@ PAGED_HD int paged_tile_start(const PagedTiles& t, int i) {
 PAGED_HD bool paged_seen(int key, int place, int window, int n_sink) {
   return key <= place && (window <= 0 || key > place - window || key < n_sink);
 }
+// Whether a row at one of the places p0 .. p1 sees one of the 16 keys from `key` on.
+PAGED_HD bool paged_span_seen(int key, int p0, int p1, int window, int n_sink) {
+  return key <= p1 && (window <= 0 || key + 15 > p0 - window || key < n_sink);
+}
 
 __device__ __forceinline__ void paged_report(const PagedView& v) {
   __hip_atomic_fetch_or(v.tickets + AF_TICKET_ERR, (int)AF_DEVERR_PAGED, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);

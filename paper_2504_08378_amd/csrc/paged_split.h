@@ -213,7 +213,9 @@ __device__ __forceinline__ void paged_split_body(const PagedSplitParams& p, cons
       }
       const bool inside = k0 + SPL_STEP - 1 <= p0 && (window <= 0 || k0 > p1 - window || k0 + SPL_STEP <= n_sink);
       if (!inside || bad[0] || bad[1]) {
-        if (bad[0] || bad[1]) paged_report(v);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)  // (a step may hold keys that no row sees, with or without a page)
+          if (bad[i] && paged_span_seen(k0 + i * 16, p0, p1, window, n_sink)) paged_report(v);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
           if (bad[j >> 2] || !paged_seen(k0 + (j >> 2) * 16 + g * 4 + (j & 3), place, window, n_sink)) sc[j] = -INFINITY;

@@ -38,3 +38,24 @@ def test_weights_of_prompts_in_fp16_where_the_caller_says_so(ctx):
     check(coarse, attend(bt, q, heads), heads, hd, weights16=True)
     assert not np.array_equal(coarse, fine) and np.array_equal(coarse[300], fine[300])
     assert np.array_equal(run(ctx, bt, heads, q=q)[1], fine)
+
+
+@pytest.mark.parametrize("page", [16, 32])
+@pytest.mark.parametrize("new", [1, 2, 40])
+@pytest.mark.parametrize("window,sinks", [(100, 4), (100, 16), (100, 17), (100, 40), (31, 4), (33, 1), (16, 0), (1, 33)])
+def test_pages_that_no_token_needs_may_be_gone(ctx, page, new, window, sinks):
+    """Pages between the first tokens and the window, given back: entries that hold nothing are neither seen nor reported."""
+    heads, kv, hd = 4, 2, 64
+    lens = [(new + past, new) for past in (300, 47, 48, 63, 64, 130)]
+    bt = Batch(lens, kv, hd, page, seed=window + sinks, single=new == 1)
+    gone = 0
+    for b, (n, q) in enumerate(lens):
+        j = np.arange(n)
+        seen = (j > n - q - window) | (j < sinks)
+        for e in range(-(-n // page)):
+            if not np.any(seen[e * page: (e + 1) * page]):
+                bt.table[b, e] = -1
+                gone += 1
+    assert gone
+    q, got = run(ctx, bt, heads, window=window, n_sink=sinks)
+    check(got, attend(bt, q, heads, window, sinks), heads, hd)
