@@ -268,7 +268,7 @@ class PagedBatch:
         if page_table.get_device() != self.index or (q_start is not None and q_start.get_device() != self.index):
             raise TypeError("the tensors of a batch must be on one device")
         self.struct = PagedBatchStruct(
-            n_seqs, page_table.shape[1], self.n_rows, int(self.n_rows if max_q_len is None else max_q_len),
+            n_seqs, page_table.shape[1], self.n_rows, int(max(self.n_rows, 1) if max_q_len is None else max_q_len),
             _ptr(page_table, torch.int32, "page_table"), _ptr(kv_len, torch.int32, "kv_len"),
             _ptr(q_start, torch.int32, "q_start"))
         self._ref = C.byref(self.struct)

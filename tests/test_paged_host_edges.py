@@ -1,0 +1,28 @@
+"""Host side of the paged operators on the CPU, where their arguments have edges."""
+import os
+
+import pytest
+import torch
+
+from paper_2504_08378_amd import binding as B
+from paper_2504_08378_amd import build
+from test_paged_refusals import EWORKSPACE, _append, _attention
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    if not os.path.exists(B.LIB_PATH):
+        build.build(verbose=False)
+
+
+def test_a_batch_without_rows_is_one(monkeypatch):
+    """n_rows 0 without max_q_len: the bound is one row, as every call wants it."""
+    monkeypatch.setattr(B, "_ptr", lambda t, *a: None if t is None else t.data_ptr())
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    s = B.PagedBatch(i32(3, 5), i32(3), i32(4), n_rows=0).struct
+    batch = {n: getattr(s, n) for n, _ in B.PagedBatchStruct._fields_}
+    for call in (_append, _attention):
+        assert call(batch=batch) == EWORKSPACE   # past every check
+    assert B.PagedBatch(i32(3, 5), i32(3), i32(4), n_rows=7).struct.max_q_len == 7
+    assert B.PagedBatch(i32(3, 5), i32(3), i32(4), n_rows=7, max_q_len=4).struct.max_q_len == 4
+    assert B.PagedBatch(i32(3, 5), i32(3)).struct.max_q_len == 1
