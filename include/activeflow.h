@@ -369,7 +369,7 @@ int af_paged_append(af_ctx* ctx, const af_paged_cache* cache, const af_paged_bat
  * tokens j <= p (window == 0), or those of them with j > p - window or j < n_sink (the last
  * `window`, and the first n_sink).
  *   out = sum of softmax(scale * q.k_j) v_j over the tokens it sees, 0 if there are none
- * (scale 0: 1 / sqrt(head_dim)).  Scores, softmax and sums are fp32; the weights enter the value products as two fp16 values
+ * (scale 0: 1 / sqrt(head_dim); scale * log2(e) has to be finite).  Scores, softmax and sums are fp32; the weights enter the value products as two fp16 values
  * (22 bits), unless AF_OPT_PAGED_F16_WEIGHTS is set.  Tokens that a row does not see do not enter its result, whatever their key and value hold.  The result depends on
  * the batch (the work is divided by its lengths) within rounding, and is the same from call to call.
  * Alignment, device and workspace as af_paged_append; out must not overlap q. */

@@ -94,8 +94,9 @@ extern "C" int af_paged_attention(af_ctx* ctx, const af_paged_cache* cache, cons
   int rc = af_paged_view(cache, batch, n_heads, &p.v);
   if (rc != AF_OK) return rc;
   if ((!q_f16 || !out_f16) && batch->n_rows) return AF_ENULL;
-  if (window < 0 || n_sink < 0 || !(fabsf(scale) < INFINITY)) return AF_EINVAL;
   const int hd = cache->head_dim;
+  p.scale2 = (scale == 0.f ? 1.0f / sqrtf((float)hd) : scale) * 1.44269504088896340736f;
+  if (window < 0 || n_sink < 0 || !(fabsf(p.scale2) < INFINITY)) return AF_EINVAL;
   if (!af_paged_rows_ok(q_f16, q_stride, (long long)n_heads * hd) ||
       !af_paged_rows_ok(out_f16, out_stride, (long long)n_heads * hd))
     return AF_ESHAPE;
@@ -108,6 +109,5 @@ extern "C" int af_paged_attention(af_ctx* ctx, const af_paged_cache* cache, cons
   p.n_heads = n_heads;
   p.window = window;
   p.n_sink = window > 0 ? n_sink : 0;
-  p.scale2 = (scale == 0.f ? 1.0f / sqrtf((float)hd) : scale) * 1.44269504088896340736f;
   return hd == 128 ? launch_attention<128>(ctx, p) : launch_attention<64>(ctx, p);
 }

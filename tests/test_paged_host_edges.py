@@ -6,7 +6,7 @@ import torch
 
 from paper_2504_08378_amd import binding as B
 from paper_2504_08378_amd import build
-from test_paged_refusals import EWORKSPACE, _append, _attention
+from test_paged_refusals import EINVAL, EWORKSPACE, _append, _attention
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -26,3 +26,12 @@ def test_a_batch_without_rows_is_one(monkeypatch):
     assert B.PagedBatch(i32(3, 5), i32(3), i32(4), n_rows=7).struct.max_q_len == 7
     assert B.PagedBatch(i32(3, 5), i32(3), i32(4), n_rows=7, max_q_len=4).struct.max_q_len == 4
     assert B.PagedBatch(i32(3, 5), i32(3)).struct.max_q_len == 1
+
+
+def test_scales_at_the_end_of_the_range():
+    """The kernels work with scale * log2(e): both have to be finite."""
+    largest = float(torch.finfo(torch.float32).max)
+    for scale in (largest, -largest, 2.5e38):
+        assert _attention(scale=scale) == EINVAL
+    for scale in (2.3e38, -2.3e38, 1e-38):
+        assert _attention(scale=scale) == EWORKSPACE
