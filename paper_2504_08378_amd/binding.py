@@ -514,11 +514,13 @@ class Context:
     def decode_layer_batch_paged(self, cfg: LayerCfg, w: LayerWeights, hidden_in, hidden_out, cache: PagedCache,
                                  batch: PagedBatch, sel: SelectCfg, sets: IdxSets, union_n=None, pos=None, window: int = 0,
                                  n_sink: int = 0, q_gain=None, k_gain=None):
-        """decode_layer_batch over a paged cache: hidden_in / hidden_out fp16 [batch.n_rows][d]."""
+        """decode_layer_batch over a paged cache: hidden_in / hidden_out fp16 [batch.n_rows][d]; union_n int32 [4]."""
         self._paged_check(cache, batch)
         for t, name in ((hidden_in, "hidden_in"), (hidden_out, "hidden_out")):
-            if t.numel() != batch.n_rows * cfg.d_model:
-                raise TypeError(f"{name} must be [{batch.n_rows}][{cfg.d_model}]")
+            if t.numel() != batch.n_rows * cfg.d_model or t.get_device() != self.device.index:
+                raise TypeError(f"{name} must be [{batch.n_rows}][{cfg.d_model}] on the context's device")
+        if union_n is not None and (union_n.numel() < 4 or union_n.get_device() != self.device.index):
+            raise TypeError("union_n must have 4 entries on the context's device")
         self._paged_extras(batch, cache.head_dim, q_gain, k_gain, pos)
         _check(lib().af_decode_layer_batch_paged(
             self._h, C.byref(cfg), C.byref(w), _ptr(hidden_in, torch.float16, "hidden_in"),
