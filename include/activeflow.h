@@ -330,7 +330,7 @@ typedef struct {
 
 /* The sequences of one call and their new tokens.  All pointers are device memory.
  *   page_table [n_seqs][table_stride]: page of tokens [i * page_tokens, (i + 1) * page_tokens) of
- *     a sequence at entry i; entries behind a sequence's last token are not read.
+ *     a sequence at entry i; what entries behind a sequence's last token hold does not matter.
  *   kv_len [n_seqs]: tokens of each sequence, the new ones included.
  *   q_start [n_seqs + 1]: the new tokens of sequence b are rows [q_start[b], q_start[b+1]) of the
  *     token tensors, its last q_start[b+1] - q_start[b] (0 or more, at most kv_len[b]) tokens in
@@ -383,7 +383,8 @@ int af_paged_attention(af_ctx* ctx, const af_paged_cache* cache, const af_paged_
  * the heads' norms (as af_paged_append, with cfg's rms_eps), or NULL for none.  All lengths are device memory: a captured step
  * goes on being valid while the sequences grow.  The rotated queries are rounded to fp16 between the two operators;
  * otherwise a token's result is what af_decode_layer_batch gives for it.  Rows without a token (padding, reported ranges) get
- * values without meaning, the others' do not depend on them. */
+ * values without meaning; the others' results do not depend on what those hold, NaN and infinities included, beyond rounding (all
+ * rows' channels make up the union, whose parts are summed one after another). */
 int af_decode_layer_batch_paged(af_ctx* ctx, const af_layer_cfg* cfg, const af_layer_weights* w,
                                 const void* hidden_in, void* hidden_out, const af_paged_cache* cache,
                                 const af_paged_batch* batch, const int32_t* pos, int window, int n_sink,
