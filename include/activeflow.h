@@ -341,7 +341,8 @@ typedef struct {
  * A table entry outside [0, n_pages) that a token needs, a negative kv_len or one beyond the
  * table, a row range that is negative, outside [0, n_rows], longer than max_q_len or than kv_len:
  * reported (AF_DEVERR_PAGED) and not followed.  The token of such an entry is not stored and not
- * seen; the rows of such a sequence are left as they are. */
+ * seen; the rows of such a sequence are left as they are (where the ranges around it then overlap, the rows that
+ * these share hold either's result or stay). */
 enum { AF_PAGED_MAX_SEQS = 1024, AF_PAGED_MAX_HEADS = 1024, AF_PAGED_MAX_ROWS = 1 << 22, AF_PAGED_MAX_TOKENS = 1 << 30 };
 typedef struct {
   int n_seqs, table_stride, n_rows, max_q_len;
