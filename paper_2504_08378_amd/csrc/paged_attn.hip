@@ -60,8 +60,8 @@ static int launch_attention(af_ctx* ctx, const PagedAttnParams& a) {
   const long long longer = a.v.n_rows / (short_q + 1);
   const long long longs = ((long long)a.v.n_rows * rep / PRM_ROWS + (a.v.n_seqs < longer ? a.v.n_seqs : longer)) * a.v.n_kv;
   // In pieces where they would not fill the chip, two a unit, and the keys may be many (us, whole / in pieces, 32 query heads on 8:
-  // 32 tokens behind 8000 147 / 40, 256 behind 30000 539 / 192, two times 64 behind 2000 44.5 / 25.9; 16 on 1, 100 behind 60000 1046 / 96;
-  // where the keys are few there is one piece: 500 tokens 16.6 / 17.0).
+  // 32 tokens behind 8000 195 / 43, 256 behind 30000 712 / 252, two times 64 behind 2000 57.0 / 29.0; 16 on 1, 100 behind 60000 1398 / 119;
+  // where the keys are few there is one piece: 500 tokens 19.8).
   PagedPieces pieces{};
   pieces.tickets = p.tickets;
   pieces.ticket0 = 2 * SPL_MAX_WGS;

@@ -12,16 +12,17 @@
 // that order.
 //
 // The weights enter the value products as two fp16 values, 22 bits, so these are formed twice: 1.5 times the matrix work of weights
-// rounded to fp16, which leave the results 2.6e-4 from 64 bits where their own rounding leaves 2.0e-4.  The caller may choose those
-// (FINE false).
+// rounded to fp16, which leave the results up to 2.6e-4 from 64 bits where their own rounding leaves 2.0e-4.  The caller may choose
+// those (FINE false).
 //
-// What bounds it, 8192 tokens of 32 heads on 32, causal, 550 GFLOP: 765 us, 1080 TFLOP/s with the second value products; rounded weights
-// 580 us.  The matrix unit at the clock that power allows (a loop of nothing but these instructions on random data runs at 1.6 GHz,
-// 1650 TFLOP/s, and at 2.1 GHz on zeros), and the time when neither of the two waves of a SIMD has products ready.  On the way, us, with rounded
-// weights: all loads of a tile issued in a row at its start, where a wave waits until the memory path has taken them, and each read next
-// to its product 669; a maximum per tile and an exchange between the lanes 655; loads between the products, with reads that the compiler
-// could not tell from the loads' buffers (it waited for them) 667; this form 573.  Eight waves on one pair of tiles, half of them a phase
-// behind the others, 573; without the waves' priorities 587.
+// What bounds it, 8192 tokens of 32 heads on 32, causal, 550 GFLOP and 275 more for the second value products: 762 us, 1080 TFLOP/s; the
+// matrix unit is busy 64 % of the cycles, and the clock is the 1.58 GHz that power allows.  Rounded weights: 581 us, 51 % at 1.73 GHz.  (A
+// loop of nothing but these instructions on random data runs at 1.6 GHz, 1650 TFLOP/s, and at 2.1 GHz on zeros.)  In the other cycles
+// neither of the two waves of a SIMD has products ready.  On the way, us, with rounded weights: all loads of a tile issued in a row at its
+// start, where a wave waits until the memory path has taken them, and each read next to its product 669; a maximum per tile and an
+// exchange between the lanes 655; loads between the products, with reads that the compiler could not tell from the loads' buffers (it
+// waited for them) 667; this form 573.  Eight waves on one pair of tiles, half of them a phase behind the others, 573; without the
+// waves' priorities 587.
 #pragma once
 #include <type_traits>
 
@@ -140,7 +141,7 @@ __device__ __forceinline__ void paged_prompt_body(const PagedAttnParams& p, cons
   };
 
   // The first tile's keys and values and the second's keys are requested together; the first step waits for the first keys only
-  // (8932 rows that see 1028 keys each, us: with only the keys at first 181.4, so 178.3).
+  // (8932 rows that see 1028 keys each, rounded weights, us: with only the keys at first 181.4, so 178.3).
   if (tid == 0) s_gone = 0;
   id_next = page_of(t0);
   const int id_second = page_of(t0 + 1);
