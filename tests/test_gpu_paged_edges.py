@@ -77,6 +77,16 @@ def test_many_sequences_and_a_prompt_at_width_128(ctx, seqs):
         check(got, attend(bt, q, heads, window, sinks), heads, hd, untouched=5.0)
 
 
+@pytest.mark.parametrize("heads,kv,hd", [(8, 2, 64), (32, 8, 128)])
+def test_a_chunk_behind_a_long_past_among_single_tokens(ctx, heads, kv, hd):
+    """A serving step of chunked prompts: one request's next 100 tokens behind 2500, the others one token each."""
+    lens = [(1 + 37 * i % 300, 1) for i in range(40)]
+    lens[23] = (2600, 100)
+    bt = Batch(lens, kv, hd, 16, seed=heads)
+    q, got = run(ctx, bt, heads)
+    check(got, attend(bt, q, heads), heads, hd)
+
+
 # ---- padded batches through the layer --------------------------------------------------------------------
 def _hidden(shape, n, first=0):
     scales = S.channel_scales(0, shape.d_model, shape.name)
